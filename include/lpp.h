@@ -366,6 +366,140 @@ int32_t lpp_commit_kv(const lpp_tree* tree, int32_t dtype, const void* k_tree, c
                       int32_t B, int32_t H, int32_t S, int32_t Dh, void* k_cache, void* v_cache,
                       int32_t* new_len, void* stream);
 
+/* ----------------------------------------------------------- paged cache ---
+ * A key/value cache in pages, for batches whose sequences grow apart: the same step over it as over the contiguous
+ * caches above (the paper verifies one sequence, App. A.2; nothing of the method depends on where a key lies).
+ *   k_pages, v_pages  [device] [n_pages, Hkv, page_size, Dh], 16-byte aligned; one pair for every layer
+ *   page_table        [device] int32 [B, table_stride]: position p of item b lies in slot p % page_size of page
+ *                     page_table[b, p / page_size]
+ * Pages may be shared by items that only read them; a page that is written (commit, append) belongs to one item.
+ * Reads clamp a table entry to [0, n_pages); writes leave a position out whose entry lies outside.  Slots that hold no position yet may
+ * hold anything, NaN included.
+ * The handle holds the geometry and a few words that the attention's blocks leave for each other: attention calls that
+ * share a handle (the layers of a model may) must be ordered on a stream, two captured graphs of them as well; work that may
+ * overlap takes a handle of its own.  With no HIP device present the handle is host-only, as a tree's.
+ *   page_size   16, 32, 64, 128 or 256;  Dh 64 or 128;  Hkv at most 4096
+ * Calls whose handle was made on another device than the current one return LPP_EINVAL (these, and those of the two sections below).
+ * Errors: LPP_EINVAL (null, sizes < 1), LPP_EUNSUPPORTED (dtype, Dh, page_size or Hkv outside the above), LPP_EHIP.
+ */
+typedef struct lpp_paged lpp_paged;
+int32_t lpp_paged_create(int32_t dtype, int32_t Hkv, int32_t Dh, int32_t page_size, int32_t n_pages, lpp_paged** out);
+int32_t lpp_paged_destroy(lpp_paged* cache);
+
+/* lpp_commit_kv over pages: row 0 and the accepted path's rows of k_tree / v_tree [device] [B, Hkv, M, Dh] go to positions
+ * seq_len[b], seq_len[b] + 1, ...; new_len[b] = seq_len[b] + 1 + accept_len[b].  Capacity is table_stride * page_size: rows
+ * at or past it are dropped, lengths are clamped to it.  new_len may be NULL and must not be seq_len itself.
+ * lpp_paged_append_kv: rows 0 .. row_len[b] - 1 of k_new / v_new [device] [B, Hkv, M, Dh] instead (a chunk of a prompt);
+ * row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M for every item).
+ * Errors: LPP_EINVAL (null, sizes < 1, new_len == seq_len, tensors not 16-byte aligned), LPP_EUNSUPPORTED (capacity + M or the
+ * launch's blocks beyond 2^31), LPP_EHIP.
+ */
+int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* tree, const void* k_tree, const void* v_tree,
+                            const int32_t* path, const int32_t* accept_len, const int32_t* page_table,
+                            int32_t table_stride, const int32_t* seq_len, int32_t B, void* k_pages, void* v_pages,
+                            int32_t* new_len, void* stream);
+int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const void* v_new, const int32_t* row_len,
+                            const int32_t* page_table, int32_t table_stride, const int32_t* seq_len, int32_t B,
+                            int32_t M, void* k_pages, void* v_pages, int32_t* new_len, void* stream);
+
+/* -------------------------------------------------------- rotary positions ---
+ * Between a layer's projections and its attention: queries and keys of a step's rows are turned by their positions,
+ * values go along, and all three come out in the layouts that attention and commit read.
+ *   row (b, i) stands at first_pos[b] + depth of row i (tree given: its rows) or first_pos[b] + i (tree NULL: a chunk)
+ *   pair j of the first `dim` numbers of a head, (x1, x2) = (x[j], x[j + dim/2]) (LPP_ROTARY_HALF) or (x[2j], x[2j + 1])
+ *   (LPP_ROTARY_INTERLEAVED), becomes  m (x1 cos a - x2 sin a), m (x2 cos a + x1 sin a)  with a = position * theta_j; the
+ *   other numbers of a head, and the values, are copied.
+ *   theta_j = base^(-2j / dim);  LPP_ROTARY_LINEAR: theta_j / factor;  LPP_ROTARY_NTK: base * factor^(dim / (dim - 2)) for
+ *   base;  LPP_ROTARY_YARN: with r = original_len * theta_j / (2 pi) turns and g = clamp((r - slow) / (fast - slow), 0, 1),
+ *   (1 - g) theta_j / factor + g theta_j, and m = 0.1 ln(factor) + 1.  m = 1 otherwise; `magnitude` > 0 sets m.
+ * Angles are formed in float64 and reduced before they are rounded: far positions are as exact as near ones.
+ *   lpp_rotary_config   dim a multiple of 16 up to LPP_ROTARY_MAX_DIM; zeros select base 10000, fast 32, slow 1;
+ *                       factor >= 1 (not read without scaling); original_len >= 1 (read by YARN only)
+ *   lpp_rows            a projection's output: number d of head h of row (b, i) is element b item + i row + h head + d
+ *                       of `data` [device]; strides in elements, multiples of 16 bytes, none negative; 16-byte aligned
+ *   q, k, v             [host] read during the call only; any may be NULL together with its output; H heads of q, Hkv of k and v
+ *   first_pos           [device] int32 [B] or NULL (= 0);  row_len [device] int32 [B] or NULL: rows behind an item's
+ *                       last are not written
+ *   q_out [B, H, M, Dh], k_out and v_out [B, Hkv, M, Dh]   [device] contiguous, 16-byte aligned; an output may be its input
+ *                       if the strides are the output's, and must not overlap one otherwise
+ * The handle lives on the host (it may be used on any device).  Errors: LPP_EINVAL (null, sizes < 1, tree of another M, dim > Dh,
+ * an unknown enumerator, a config out of range, misaligned or partly overlapping in place), LPP_EUNSUPPORTED (dtype, dim or Dh not a multiple of
+ * 16 or too large, strides not multiples of 16 bytes), LPP_EHIP.
+ */
+#define LPP_ROTARY_MAX_DIM     256
+#define LPP_ROTARY_HALF        0
+#define LPP_ROTARY_INTERLEAVED 1
+#define LPP_ROTARY_NONE        0
+#define LPP_ROTARY_LINEAR      1
+#define LPP_ROTARY_NTK         2
+#define LPP_ROTARY_YARN        3
+typedef struct lpp_rotary lpp_rotary;
+typedef struct lpp_rotary_config {
+  int32_t dim;
+  int32_t layout;
+  int32_t scaling;
+  int32_t original_len;
+  double  base;
+  double  factor;
+  double  fast;
+  double  slow;
+  double  magnitude;
+} lpp_rotary_config;
+typedef struct lpp_rows {
+  const void* data;
+  int64_t item, row, head;
+} lpp_rows;
+int32_t lpp_rotary_create(const lpp_rotary_config* config, lpp_rotary** out);
+int32_t lpp_rotary_destroy(lpp_rotary* rotary);
+int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree, int32_t dtype, const lpp_rows* q,
+                       const lpp_rows* k, const lpp_rows* v, const int32_t* first_pos, const int32_t* row_len,
+                       int32_t B, int32_t H, int32_t Hkv, int32_t M, int32_t Dh, void* q_out, void* k_out,
+                       void* v_out, void* stream);
+
+/* ------------------------------------------------------- logits of a step ---
+ * What sampling settings do to the target's logits ahead of verification (App. B "Models" has guidance and top-k;
+ * penalties, biases and masks are what serving adds).  Row i of item b is judged in the context of its own path:
+ *   l = u + cfg_scale (c - u) with unconditional logits, else l = c;      c = logits[b, i, vocab_offset + x]
+ *   n = counts[b, x] + how often x is drafted on the path from the root to row i (row i included, the root not: its token
+ *       is history)
+ *   n > 0:  l = (l > 0 ? l / repetition[b] : l * repetition[b]) - frequency[b] n - presence[b]
+ *   l = l + bias[x];   l = -inf where bit x % 32 of word x / 32 of the row's mask is 0, whatever l was
+ * in float32; out[b, i, vocab_offset + x] = l.  Columns outside [vocab_offset, vocab_offset + V) are neither read nor
+ * written.  A row whose mask allows nothing is -inf throughout: it has no distribution, and lpp_relaxed_verify wants one.
+ *   logits, uncond_logits   [device] [B, M, ldv], float32 or bf16 (dtype);  out [device] float32 [B, M, ldv], which may be
+ *                           either of the two where they are float32
+ *   tokens    [device] int32 [B, M] as for lpp_relaxed_verify (clamped to [0, V)), or NULL: paths count nothing
+ *   counts    [device] int32 [B, V] or NULL;   repetition, frequency, presence   [device] float32 [B] or NULL (= 1, 0, 0)
+ *   bias      [device] float32, row b at bias + b * bias_stride (0: one row for all), or NULL
+ *   mask      [device] uint32, row (b, i) at mask + b * mask_item_stride + i * mask_row_stride, ceil(V / 32) words, or NULL
+ * lpp_token_counts    counts[b, x] = how often x occurs among the first len[b] (NULL: T) of tokens [device] int32 [B, T];
+ *                     what lies outside [0, V) counts nowhere.  Whatever was in counts is overwritten.
+ * lpp_commit_counts   adds what a step emitted: the tokens of the accepted path and final_token, as lpp_relaxed_verify wrote
+ *                     them (an item whose walk gave up adds nothing).
+ * Errors: LPP_EINVAL (null, sizes < 1, vocab_offset < 0, vocab_offset + V > ldv, cfg_scale NaN, negative strides, bf16 in place),
+ * LPP_EUNSUPPORTED (dtype unknown, launch beyond 2^31 blocks), LPP_EHIP.
+ */
+typedef struct lpp_logits_options {
+  const void*     uncond_logits;
+  const int32_t*  tokens;
+  const int32_t*  counts;
+  const float*    repetition;
+  const float*    frequency;
+  const float*    presence;
+  const float*    bias;
+  const uint32_t* mask;
+  int64_t         bias_stride;
+  int64_t         mask_item_stride;
+  int64_t         mask_row_stride;
+  float           cfg_scale;
+} lpp_logits_options;
+int32_t lpp_adjust_logits(const lpp_tree* tree, int32_t dtype, const void* logits, int64_t ldv, int32_t vocab_offset,
+                          int32_t V, int32_t B, const lpp_logits_options* opts, float* out, void* stream);
+int32_t lpp_token_counts(const int32_t* tokens, const int32_t* len, int32_t B, int32_t T, int32_t V, int32_t* counts,
+                         void* stream);
+int32_t lpp_commit_counts(const lpp_tree* tree, const int32_t* tokens, const int32_t* path, const int32_t* accept_len,
+                          const int32_t* final_token, int32_t B, int32_t V, int32_t* counts, void* stream);
+
 /* ----------------------------------------------------------------- probe ---
  * Measurement aid, not a step of the method: streams `bytes` (rounded down to a multiple of 16)
  * from src once with `blocks` workgroups of 256 lanes and writes nothing (sink may be NULL; it is

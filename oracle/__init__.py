@@ -36,6 +36,14 @@ Functions and what pins them (see tests/test_oracle_*.py):
                     (App. B "Models").  Pinned by special cases (scale 0, equal rows),
                     a library top-k, counts and brute force.
 
+  paged_attention, paged_write   the same attention and commit over a cache in pages, and causal
+                    chunks.  Pinned by the contiguous oracles on gathered pages.
+
+  rotary_angles, rotate   rotary positions of queries and keys.  Pinned by products that depend on
+                    distances alone and by hand values.
+
+  adjust_logits     penalties, biases and masks along a row's path.  Pinned by special cases and counts.
+
 Readings the paper does not fix ("parity unpinned": every invariant the paper
 states holds under the alternatives too, so the choice below is the definition):
   * A_{k,lambda} is the longest nearest-first prefix of B_k whose cumulative
@@ -58,3 +66,6 @@ from .verify import relaxed_verify, softmax64, inverse_cdf    # noqa: F401
 from .f32_bound import float32_error_bound                    # noqa: F401
 from .commit import commit_kv                                 # noqa: F401
 from .frontend import guided_logits, top_k_filter, sampling_frontend   # noqa: F401
+from .paged import gather_pages, paged_attention, paged_write  # noqa: F401
+from .rotary import rotary_angles, rotate                     # noqa: F401
+from .logits import adjust_logits                             # noqa: F401

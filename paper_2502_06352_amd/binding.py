@@ -84,6 +84,20 @@ def lib() -> C.CDLL:
                                           C.POINTER(VerifyOut), vp, sz, vp]
     L.lpp_commit_kv.restype = i32
     L.lpp_commit_kv.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+    L.lpp_paged_create.restype = i32; L.lpp_paged_create.argtypes = [i32, i32, i32, i32, i32, C.POINTER(vp)]
+    L.lpp_paged_destroy.restype = i32; L.lpp_paged_destroy.argtypes = [vp]
+    L.lpp_paged_commit_kv.restype = i32
+    L.lpp_paged_commit_kv.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp]
+    L.lpp_paged_append_kv.restype = i32
+    L.lpp_paged_append_kv.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp]
+    L.lpp_rotary_create.restype = i32; L.lpp_rotary_create.argtypes = [vp, C.POINTER(vp)]
+    L.lpp_rotary_destroy.restype = i32; L.lpp_rotary_destroy.argtypes = [vp]
+    L.lpp_rotary_qkv.restype = i32
+    L.lpp_rotary_qkv.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+    L.lpp_adjust_logits.restype = i32
+    L.lpp_adjust_logits.argtypes = [vp, i32, vp, i64, i32, i32, i32, vp, vp, vp]
+    L.lpp_token_counts.restype = i32; L.lpp_token_counts.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+    L.lpp_commit_counts.restype = i32; L.lpp_commit_counts.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp]
     L.lpp_probe_stream_read.restype = i32
     L.lpp_probe_stream_read.argtypes = [vp, sz, vp, i32, vp]
     # (the wrappers below pass lpp_verify_out as packed bytes, through function objects of their own: who calls
@@ -302,6 +316,196 @@ def lpp_relaxed_verify_sampled(tree: Tree, cond_logits, uncond_logits, cfg_scale
                                        _verify_out(out), _ptr(ws),
                                        _bytes(ws), _stream(stream)),
            "lpp_relaxed_verify_sampled")
+
+
+# The calls below take tensors of the shapes that include/lpp.h states and say so if one is of another size or type, lies
+# on another device than the current one, or has gaps: the kernels go by sizes alone.
+_DTYPES = None
+
+
+def _device() -> int:
+    """The current HIP device, and the element types by their number."""
+    global _torch, _DTYPES
+    if _DTYPES is None:
+        import torch
+        _torch = torch
+        _DTYPES = {LPP_F32: torch.float32, LPP_BF16: torch.bfloat16, "i32": torch.int32, "f32": torch.float32}
+    c = _torch.cuda
+    return c.current_device() if c.is_initialized() or c.is_available() else -1
+
+
+def _on(stream, device: int) -> Optional[int]:
+    return None if device < 0 and stream is None else _stream(stream)
+
+
+def _refuse(where: str, what: str):
+    raise LppError(LPP_EINVAL, f"{where}: {what}")
+
+
+def _want(where: str, name: str, t, dtype, n: int, device: int) -> int:
+    """Address of ``t``, which is to be ``n`` contiguous elements on ``device``."""
+    if t.get_device() != device:
+        _refuse(where, f"{name} is not on the current device")
+    if t.dtype is not _DTYPES.get(dtype):
+        _refuse(where, f"{name} has the wrong element type")
+    if t.numel() != n or not t.is_contiguous():
+        _refuse(where, f"{name} has another size, or gaps")
+    return t.data_ptr()
+
+
+def _maybe(where: str, name: str, t, dtype, n: int, device: int) -> Optional[int]:
+    return None if t is None else _want(where, name, t, dtype, n, device)
+
+
+class PagedCache:
+    """Owner of an ``lpp_paged*``: the geometry of a key/value cache in pages."""
+
+    def __init__(self, dtype: int, Hkv: int, Dh: int, page_size: int, n_pages: int):
+        self.dtype, self.Hkv, self.Dh, self.page_size, self.n_pages = dtype, Hkv, Dh, page_size, n_pages
+        self.pool = n_pages * Hkv * page_size * Dh
+        self.handle = C.c_void_p()
+        _check(lib().lpp_paged_create(dtype, Hkv, Dh, page_size, n_pages, C.byref(self.handle)), "lpp_paged_create")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().lpp_paged_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+
+def _table(where: str, page_table, B: int, device: int) -> int:
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        _refuse(where, "page_table is not [B, table_stride]")
+    return _want(where, "page_table", page_table, "i32", page_table.numel(), device)
+
+
+def lpp_paged_commit_kv(cache: PagedCache, tree: Tree, k_tree, v_tree, path, accept_len, page_table, seq_len, B: int,
+                        k_pages, v_pages, new_len, stream=None) -> None:
+    w, d, t = "lpp_paged_commit_kv", _device(), cache.dtype
+    n = B * cache.Hkv * tree.M * cache.Dh
+    if tree.depth and path.numel() != B * tree.depth:
+        _refuse(w, "path is not [B, depth]")
+    _check(lib().lpp_paged_commit_kv(
+        cache.handle, tree.handle, _want(w, "k_tree", k_tree, t, n, d), _want(w, "v_tree", v_tree, t, n, d),
+        _want(w, "path", path, "i32", path.numel(), d) or _ptr(accept_len), _want(w, "accept_len", accept_len, "i32", B, d),
+        _table(w, page_table, B, d), page_table.shape[1], _want(w, "seq_len", seq_len, "i32", B, d), B,
+        _want(w, "k_pages", k_pages, t, cache.pool, d), _want(w, "v_pages", v_pages, t, cache.pool, d),
+        _maybe(w, "new_len", new_len, "i32", B, d), _on(stream, d)), w)
+
+
+def lpp_paged_append_kv(cache: PagedCache, k_new, v_new, row_len, page_table, seq_len, B: int, M: int, k_pages, v_pages,
+                        new_len, stream=None) -> None:
+    w, d, t = "lpp_paged_append_kv", _device(), cache.dtype
+    n = B * cache.Hkv * M * cache.Dh
+    _check(lib().lpp_paged_append_kv(
+        cache.handle, _want(w, "k_new", k_new, t, n, d), _want(w, "v_new", v_new, t, n, d),
+        _maybe(w, "row_len", row_len, "i32", B, d), _table(w, page_table, B, d), page_table.shape[1],
+        _want(w, "seq_len", seq_len, "i32", B, d), B, M, _want(w, "k_pages", k_pages, t, cache.pool, d),
+        _want(w, "v_pages", v_pages, t, cache.pool, d), _maybe(w, "new_len", new_len, "i32", B, d), _on(stream, d)), w)
+
+
+LPP_ROTARY_HALF, LPP_ROTARY_INTERLEAVED = 0, 1
+LPP_ROTARY_NONE, LPP_ROTARY_LINEAR, LPP_ROTARY_NTK, LPP_ROTARY_YARN = range(4)
+
+
+class RotaryConfig(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("original_len", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("fast", C.c_double), ("slow", C.c_double),
+                ("magnitude", C.c_double)]
+
+
+class Rotary:
+    """Owner of an ``lpp_rotary*``: how many numbers of a head turn, in which pairs, and how fast."""
+
+    def __init__(self, dim: int, layout: int = LPP_ROTARY_HALF, scaling: int = LPP_ROTARY_NONE, factor: float = 1.0,
+                 original_len: int = 0, base: float = 0.0, fast: float = 0.0, slow: float = 0.0, magnitude: float = 0.0):
+        self.dim, self.layout = dim, layout
+        self.handle = C.c_void_p()
+        config = RotaryConfig(dim, layout, scaling, original_len, base, factor, fast, slow, magnitude)
+        _check(lib().lpp_rotary_create(C.byref(config), C.byref(self.handle)), "lpp_rotary_create")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().lpp_rotary_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+
+_pack_rows = struct.Struct("Pqqq").pack
+
+
+def _rows_in(where: str, name: str, t, dtype, B: int, M: int, heads: int, Dh: int, device: int) -> Optional[bytes]:
+    """lpp_rows of a [B, M, heads, Dh] tensor of any strides but the last."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (B, M, heads, Dh):
+        _refuse(where, f"{name} is not [B, M, heads, Dh]")
+    if t.get_device() != device or t.dtype is not _DTYPES.get(dtype):
+        _refuse(where, f"{name} is not on the current device, or of another element type")
+    item, row, head, one = t.stride()
+    if one != 1:
+        _refuse(where, f"the numbers of a head of {name} do not follow each other")
+    return _pack_rows(t.data_ptr(), item, row, head)
+
+
+def lpp_rotary_qkv(rotary: Rotary, tree: Optional[Tree], dtype: int, q, k, v, first_pos, row_len, B: int, H: int, Hkv: int,
+                   M: int, Dh: int, q_out, k_out, v_out, stream=None) -> None:
+    """``q``, ``k``, ``v``: [B, M, heads, Dh] views of the projections' output (their strides are passed on), or None."""
+    w, d = "lpp_rotary_qkv", _device()
+    _check(lib().lpp_rotary_qkv(
+        rotary.handle, None if tree is None else tree.handle, dtype, _rows_in(w, "q", q, dtype, B, M, H, Dh, d),
+        _rows_in(w, "k", k, dtype, B, M, Hkv, Dh, d), _rows_in(w, "v", v, dtype, B, M, Hkv, Dh, d),
+        _maybe(w, "first_pos", first_pos, "i32", B, d), _maybe(w, "row_len", row_len, "i32", B, d), B, H, Hkv, M, Dh,
+        _maybe(w, "q_out", q_out, dtype, B * H * M * Dh, d), _maybe(w, "k_out", k_out, dtype, B * Hkv * M * Dh, d),
+        _maybe(w, "v_out", v_out, dtype, B * Hkv * M * Dh, d), _on(stream, d)), w)
+
+
+_pack_logits = struct.Struct("8P3qf4x").pack
+
+
+def lpp_adjust_logits(tree: Tree, dtype: int, logits, ldv: int, vocab_offset: int, V: int, B: int, out, stream=None, *,
+                      tokens=None, counts=None, repetition=None, frequency=None, presence=None, bias=None, mask=None,
+                      uncond_logits=None, cfg_scale: float = 0.0) -> None:
+    """``bias``: [V] or [B, V];  ``mask``: int32 words [ceil(V/32)], [B, ceil(V/32)] (one for all rows of an item) or
+    [B, M, ceil(V/32)]."""
+    w, d, M = "lpp_adjust_logits", _device(), tree.M
+    words, n = -(-V // 32), B * M * ldv
+    b_stride = m_item = m_row = 0
+    if bias is not None and bias.dim() == 2:
+        b_stride = V
+    if mask is not None and mask.dim() > 1:
+        m_item, m_row = (words, 0) if mask.dim() == 2 else (M * words, words)
+    opts = _pack_logits(
+        _maybe(w, "uncond_logits", uncond_logits, dtype, n, d) or 0, _maybe(w, "tokens", tokens, "i32", B * M, d) or 0,
+        _maybe(w, "counts", counts, "i32", B * V, d) or 0, _maybe(w, "repetition", repetition, "f32", B, d) or 0,
+        _maybe(w, "frequency", frequency, "f32", B, d) or 0, _maybe(w, "presence", presence, "f32", B, d) or 0,
+        _maybe(w, "bias", bias, "f32", B * V if b_stride else V, d) or 0,
+        _maybe(w, "mask", mask, "i32", (B if m_item else 1) * (M if m_row else 1) * words, d) or 0,
+        b_stride, m_item, m_row, cfg_scale)
+    _check(lib().lpp_adjust_logits(tree.handle, dtype, _want(w, "logits", logits, dtype, n, d), ldv, vocab_offset, V, B, opts,
+                                   _want(w, "out", out, "f32", n, d), _on(stream, d)), w)
+
+
+def lpp_token_counts(tokens, length, B: int, V: int, counts, stream=None) -> None:
+    """``tokens``: [B, T];  ``length``: [B] or None (= T)."""
+    w, d = "lpp_token_counts", _device()
+    if tokens.dim() != 2 or tokens.shape[0] != B:
+        _refuse(w, "tokens is not [B, T]")
+    _check(lib().lpp_token_counts(_want(w, "tokens", tokens, "i32", tokens.numel(), d), _maybe(w, "length", length, "i32", B, d),
+                                  B, tokens.shape[1], V, _want(w, "counts", counts, "i32", B * V, d), _on(stream, d)), w)
+
+
+def lpp_commit_counts(tree: Tree, tokens, path, accept_len, final_token, B: int, V: int, counts, stream=None) -> None:
+    w, d = "lpp_commit_counts", _device()
+    if tree.depth and path.numel() != B * tree.depth:
+        _refuse(w, "path is not [B, depth]")
+    _check(lib().lpp_commit_counts(
+        tree.handle, _want(w, "tokens", tokens, "i32", B * tree.M, d),
+        _want(w, "path", path, "i32", path.numel(), d) or _ptr(accept_len), _want(w, "accept_len", accept_len, "i32", B, d),
+        _want(w, "final_token", final_token, "i32", B, d), B, V, _want(w, "counts", counts, "i32", B * V, d),
+        _on(stream, d)), w)
 
 
 def lpp_probe_stream_read(src, blocks: int, sink=None, stream=None) -> None:

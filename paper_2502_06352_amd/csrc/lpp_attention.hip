@@ -29,15 +29,12 @@
 #include <atomic>
 #include <type_traits>
 
+#include "lpp_device.h"
 #include "lpp_internal.h"
 #include "lpp_reciprocal.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kMasked = -1.0e30f;  // finite stand-in for -inf
@@ -92,37 +89,6 @@ __device__ __forceinline__ uint4 ld16(const char* p) { return *reinterpret_cast<
 __device__ __forceinline__ uint4 ld16(const uint16_t* p) {
   return *reinterpret_cast<const uint4*>(p);
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // round to nearest even (hardware convert)
-  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
-}
-
-// 16- and 8-byte accesses that are visible device-wide once they have completed (the cache policy
-// of a device-scope atomic, on whole vectors): what the blocks of one head exchange their partial
-// results with inside one launch.  `off` is a byte offset into the buffer behind `rsrc`.
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-constexpr int kDeviceScope = 16;     // sc1
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t device_buffer(const void* base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
-}
-__device__ __forceinline__ void store_dev(__amdgpu_buffer_rsrc_t r, uint32_t off, float4 v) {
-  const u32x4 x = {__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
-  __builtin_amdgcn_raw_buffer_store_b128(x, r, (int)off, 0, kDeviceScope);
-}
-__device__ __forceinline__ void store_dev(__amdgpu_buffer_rsrc_t r, uint32_t off, float2 v) {
-  const u32x2 x = {__float_as_uint(v.x), __float_as_uint(v.y)};
-  __builtin_amdgcn_raw_buffer_store_b64(x, r, (int)off, 0, kDeviceScope);
-}
-__device__ __forceinline__ float4 load_dev4(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-  const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, kDeviceScope);
-  return make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
-}
-__device__ __forceinline__ float2 load_dev2(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-  const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, kDeviceScope);
-  return make_float2(__uint_as_float(x.x), __uint_as_float(x.y));
-}
-
 // four consecutive output elements starting at element index e of the output tensor
 __device__ __forceinline__ void store_out4(float* out, bool as_bf16, int64_t e, float4 v) {
   if (as_bf16)
@@ -608,16 +574,6 @@ struct AttnArgsF32 {
   float4* ws_o;                     // [layer][BH][mtiles][nsplit][16][Dh]  unnormalised partial O
   float2* ws_ml;                    // [layer][BH][mtiles][nsplit][16]      (reference max, sum)
 };
-
-// e^t for t <= 0 (0 below -200, NaN stays): the hardware's 2^x on t log2 e, whose rounding is taken back to first
-// order.  Without that, scores of a few units cost a fifth of the accuracy; expf keeps it, but its registers
-// spill in the kernel (12 bytes a lane at rows of 64).
-__device__ __forceinline__ float exp_neg(float t) {
-  constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-  t = t < -200.f ? -200.f : t;
-  const float x = t * kLog2e, r = __builtin_amdgcn_exp2f(x);
-  return __builtin_fmaf(r, __builtin_fmaf(t, kLog2e, -x) * kLn2, r);
-}
 
 // One tile of 16 keys in flight.  K: lane (i, g) holds of key i the dimensions 16 t + 4 g .. + 3; V: of keys
 // 4 g + r the dimensions 64 h + 4 i .. + 3 (i = lane % 16, g = lane / 16).

@@ -45,6 +45,14 @@ constexpr int kMailWords = kMailHanded + LPP_MAX_ROWS;
 
 #define LPP_COUNTER_SLOTS 4096
 
+// Geometry of a paged cache and what its attention's launches leave for each other.
+struct lpp_paged {
+  int32_t dtype = 0, Hkv = 0, Dh = 0, page_size = 0, page_shift = 0, n_pages = 0;
+  int device = -1;                 // -1: host-only handle
+  int32_t n_cu = 256;
+  int32_t* d_counters = nullptr;   // [LPP_COUNTER_SLOTS] "last block done" tickets, zero between calls
+};
+
 #define LPP_HIP_TRY(expr)                      \
   do {                                         \
     hipError_t e_ = (expr);                    \
@@ -53,6 +61,13 @@ constexpr int kMailWords = kMailHanded + LPP_MAX_ROWS;
       return LPP_EHIP;                         \
     }                                          \
   } while (0)
+
+// Whether a handle's memory is the current device's: a kernel launched elsewhere must not be handed it.
+inline bool lpp_is_current(int device) {
+  int now = -1;
+  if (hipGetDevice(&now) != hipSuccess) (void)hipGetLastError();
+  return now == device;
+}
 
 // The largest dynamic LDS size a kernel has been enabled for so far, per device: the attribute
 // (hipFuncAttributeMaxDynamicSharedMemorySize) belongs to one device's copy of the kernel.  One

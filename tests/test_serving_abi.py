@@ -1,0 +1,196 @@
+"""Host-only checks of the calls over a paged cache, of rotary positions and of adjusted logits: what they refuse, before
+anything is enqueued (no kernel runs here)."""
+import ctypes as C
+import math
+import os
+
+import pytest
+import torch
+
+import paper_2502_06352_amd as lpp
+
+FAKE = 0x1000          # 16-byte aligned; never dereferenced
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="valid arguments end in LPP_EHIP only without a device")
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(lpp.LIB_PATH):
+        from paper_2502_06352_amd.build import build_library
+        build_library(verbose=False)
+    return lpp.lib()
+
+
+def _refusals(call, good, bad):
+    """call(**good) with one argument after the other replaced: (changes, status)."""
+    for change, status in bad:
+        got = call(**dict(good, **change))
+        assert got == status, f"{change}: {got}"
+
+
+EINVAL, EUNSUP, EHIP = lpp.LPP_EINVAL, lpp.LPP_EUNSUPPORTED, lpp.LPP_EHIP
+
+
+def test_paged_handle(L):
+    def create(dtype=lpp.LPP_BF16, Hkv=8, Dh=128, page=64, n=10):
+        h = C.c_void_p()
+        st = L.lpp_paged_create(dtype, Hkv, Dh, page, n, C.byref(h))
+        assert (st == lpp.LPP_OK) == bool(h.value)
+        L.lpp_paged_destroy(h)
+        return st
+
+    assert create() == lpp.LPP_OK
+    for page in (16, 32, 128, 256):
+        assert create(page=page) == lpp.LPP_OK
+    _refusals(create, {}, [(dict(dtype=2), EUNSUP), (dict(Hkv=0), EINVAL), (dict(Hkv=4097), EUNSUP), (dict(Dh=0), EINVAL),
+                           (dict(Dh=96), EUNSUP), (dict(page=0), EINVAL), (dict(page=8), EUNSUP), (dict(page=48), EUNSUP),
+                           (dict(page=512), EUNSUP), (dict(n=0), EINVAL)])
+    assert L.lpp_paged_create(1, 8, 128, 64, 10, None) == EINVAL
+    assert L.lpp_paged_destroy(None) == lpp.LPP_OK
+
+
+@no_gpu
+def test_paged_writes_refuse(L):
+    cache, tree = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0])
+
+    def commit(c=cache.handle, t=tree.handle, k=FAKE, v=FAKE, path=FAKE, acc=FAKE, table=FAKE, stride=3, seq=FAKE, B=2, kp=FAKE,
+               vp=FAKE, new=None):
+        return L.lpp_paged_commit_kv(c, t, k, v, path, acc, table, stride, seq, B, kp, vp, new, None)
+
+    shared = [(dict(c=None), EINVAL), (dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(table=None), EINVAL),
+              (dict(stride=0), EINVAL), (dict(seq=None), EINVAL), (dict(B=0), EINVAL), (dict(kp=None), EINVAL),
+              (dict(vp=None), EINVAL), (dict(new=FAKE), EINVAL), (dict(k=FAKE + 8), EINVAL), (dict(vp=FAKE + 2), EINVAL),
+              (dict(stride=1 << 28), EUNSUP), ({}, EHIP)]
+    _refusals(commit, {}, shared + [(dict(t=None), EINVAL), (dict(path=None), EINVAL), (dict(acc=None), EINVAL)])
+
+    def append(c=cache.handle, k=FAKE, v=FAKE, rows=None, table=FAKE, stride=3, seq=FAKE, B=2, M=5, kp=FAKE, vp=FAKE, new=None):
+        return L.lpp_paged_append_kv(c, k, v, rows, table, stride, seq, B, M, kp, vp, new, None)
+
+    _refusals(append, {}, shared + [(dict(M=0), EINVAL), (dict(M=0x7FFFFFFF), EUNSUP), (dict(rows=FAKE), EHIP)])
+
+
+def test_rotary_handle(L):
+    def create(**kw):
+        c = lpp.binding.RotaryConfig(**dict(dict(dim=64), **kw))
+        h = C.c_void_p()
+        st = L.lpp_rotary_create(C.byref(c), C.byref(h))
+        assert (st == lpp.LPP_OK) == bool(h.value)
+        L.lpp_rotary_destroy(h)
+        return st
+
+    yarn = dict(scaling=3, factor=4.0, original_len=4096)
+    for good in ({}, dict(dim=16), dict(dim=256), dict(layout=1), dict(scaling=1, factor=1.0), dict(scaling=2, factor=8.0), yarn,
+                 dict(base=500000.0), dict(magnitude=1.5)):
+        assert create(**good) == lpp.LPP_OK, good
+    _refusals(create, {}, [(dict(dim=0), EINVAL), (dict(dim=24), EUNSUP), (dict(dim=272), EUNSUP), (dict(layout=2), EINVAL),
+                           (dict(scaling=4), EINVAL), (dict(scaling=-1), EINVAL), (dict(scaling=1), EINVAL),
+                           (dict(scaling=1, factor=0.5), EINVAL), (dict(scaling=1, factor=math.nan), EINVAL),
+                           (dict(base=1.0), EINVAL), (dict(base=math.inf), EINVAL), (dict(magnitude=-1.0), EINVAL),
+                           (dict(magnitude=math.nan), EINVAL)])
+    _refusals(create, yarn, [(dict(original_len=0), EINVAL), (dict(fast=1.0), EINVAL), (dict(slow=-1.0), EINVAL),
+                             (dict(fast=math.inf), EINVAL)])
+    assert L.lpp_rotary_create(None, C.byref(C.c_void_p())) == EINVAL
+    assert L.lpp_rotary_destroy(None) == lpp.LPP_OK
+
+
+def _rows(data=FAKE, item=640, row=128, head=64):
+    return lpp.binding._pack_rows(data, item, row, head)
+
+
+@no_gpu
+def test_rotary_refuses(L):
+    rotary, tree = lpp.Rotary(64), lpp.Tree([-1, 0, 0, 1, 1])
+
+    def call(r=rotary.handle, t=tree.handle, dtype=lpp.LPP_BF16, q=_rows(), k=_rows(), v=_rows(), first=FAKE, rows=None, B=2, H=4,
+             Hkv=2, M=5, Dh=64, qo=FAKE * 2, ko=FAKE * 3, vo=FAKE * 4):
+        return L.lpp_rotary_qkv(r, t, dtype, q, k, v, first, rows, B, H, Hkv, M, Dh, qo, ko, vo, None)
+
+    _refusals(call, {}, [({}, EHIP), (dict(r=None), EINVAL), (dict(q=None, k=None, v=None, qo=None, ko=None, vo=None), EINVAL),
+                         (dict(q=None), EINVAL), (dict(vo=None), EINVAL), (dict(k=None, ko=None), EHIP), (dict(dtype=7), EUNSUP),
+                         (dict(B=0), EINVAL), (dict(H=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(M=4), EINVAL), (dict(t=None, M=0), EINVAL),
+                         (dict(Dh=48), EINVAL), (dict(Dh=72), EUNSUP), (dict(Dh=272), EUNSUP), (dict(q=_rows(data=0)), EINVAL),
+                         (dict(q=_rows(data=FAKE + 2)), EINVAL), (dict(ko=FAKE + 8), EINVAL), (dict(q=_rows(row=-64)), EINVAL),
+                         (dict(k=_rows(head=65)), EUNSUP), (dict(v=_rows(item=641)), EUNSUP),
+                         # in place: only where every number stays where it is
+                         (dict(qo=FAKE), EINVAL), (dict(q=_rows(item=4 * 5 * 64, row=64, head=5 * 64), qo=FAKE), EHIP)])
+
+
+@no_gpu
+def test_logits_refuse(L):
+    tree = lpp.Tree([-1, 0, 0])
+
+    def options(**kw):
+        names = ("uncond", "tokens", "counts", "repetition", "frequency", "presence", "bias", "mask", "bias_stride", "mask_item",
+                 "mask_row", "scale")
+        return lpp.binding._pack_logits(*[kw.get(n, 0) for n in names])
+
+    def call(t=tree.handle, dtype=lpp.LPP_F32, logits=FAKE, ldv=100, off=4, V=90, B=2, opts=options(), out=FAKE):
+        return L.lpp_adjust_logits(t, dtype, logits, ldv, off, V, B, opts, out, None)
+
+    _refusals(call, {}, [({}, EHIP), (dict(t=None), EINVAL), (dict(logits=None), EINVAL), (dict(opts=None), EINVAL), (dict(out=None), EINVAL),
+                         (dict(dtype=3), EUNSUP), (dict(V=0), EINVAL), (dict(B=0), EINVAL), (dict(off=-1), EINVAL), (dict(off=11), EINVAL),
+                         (dict(dtype=lpp.LPP_BF16), EINVAL), (dict(dtype=lpp.LPP_BF16, out=FAKE * 2), EHIP),
+                         (dict(dtype=lpp.LPP_BF16, out=FAKE * 2, opts=options(uncond=FAKE * 2)), EINVAL),
+                         (dict(opts=options(scale=math.nan)), EINVAL), (dict(opts=options(bias_stride=-1)), EINVAL),
+                         (dict(opts=options(mask_item=-1)), EINVAL), (dict(opts=options(mask_row=-1)), EINVAL),
+                         (dict(B=1 << 30), EUNSUP)])
+
+    def counts(tokens=FAKE, length=None, B=2, T=7, V=90, out=FAKE):
+        return L.lpp_token_counts(tokens, length, B, T, V, out, None)
+
+    _refusals(counts, {}, [({}, EHIP), (dict(tokens=None), EINVAL), (dict(tokens=None, T=0), EHIP), (dict(B=0), EINVAL), (dict(T=-1), EINVAL),
+                           (dict(V=0), EINVAL), (dict(out=None), EINVAL)])
+
+    def commit(t=tree.handle, tokens=FAKE, path=FAKE, acc=FAKE, final=FAKE, B=2, V=90, out=FAKE):
+        return L.lpp_commit_counts(t, tokens, path, acc, final, B, V, out, None)
+
+    _refusals(commit, {}, [({}, EHIP)] + [({n: None}, EINVAL) for n in ("t", "tokens", "path", "acc", "final", "out")] +
+              [(dict(B=0), EINVAL), (dict(V=0), EINVAL)])
+
+
+def _status(call, *args, **kw):
+    with pytest.raises(lpp.LppError) as e:
+        call(*args, **kw)
+    return e.value.status
+
+
+@no_gpu
+def test_the_binding_refuses_tensors_of_other_sizes_types_and_strides():
+    """Host tensors here: with no device they pass for the current device's, and a right call ends in LPP_EHIP."""
+    B, Hkv, M, Dh, n = 2, 2, 3, 64, 4
+    cache, tree = lpp.PagedCache(lpp.LPP_F32, Hkv, Dh, 16, n), lpp.Tree([-1, 0, 0])
+    new, pool = torch.zeros(B, Hkv, M, Dh), torch.zeros(n, Hkv, 16, Dh)
+    i32 = dict(dtype=torch.int32)
+    table, lens, path = torch.zeros(B, 2, **i32), torch.zeros(B, **i32), torch.zeros(B, tree.depth, **i32)
+
+    def commit(k=new, p=path, a=lens, t=table, s=lens, kp=pool, nl=None):
+        return _status(lpp.lpp_paged_commit_kv, cache, tree, k, new, p, a, t, s, B, kp, pool, nl)
+
+    assert commit() == EHIP
+    for bad in (dict(k=new[:1]), dict(k=new.bfloat16()), dict(k=new.transpose(2, 3).contiguous().transpose(2, 3)), dict(kp=pool[:3]),
+                dict(t=table[0]), dict(t=table.long()), dict(s=lens[:1]), dict(p=path[:, :0]), dict(a=lens.float())):
+        assert commit(**bad) == EINVAL, bad
+
+    qkv = torch.zeros(B, M, 8, Dh)
+    rotary = lpp.Rotary(32)
+    q, k, v = qkv.split([4, 2, 2], 2)
+    out = [torch.zeros(B, h, M, Dh) for h in (4, 2, 2)]
+
+    def turn(q=q, o=out[0], first=lens):
+        return _status(lpp.lpp_rotary_qkv, rotary, tree, lpp.LPP_F32, q, k, v, first, None, B, 4, 2, M, Dh, o, out[1], out[2])
+
+    assert turn() == EHIP
+    for bad in (dict(q=qkv), dict(q=q.bfloat16()), dict(q=torch.zeros(B, M, 4, 2 * Dh)[..., ::2]), dict(o=out[1]), dict(first=lens.long())):
+        assert turn(**bad) == EINVAL, bad
+
+    x = torch.zeros(B, M, 40)
+
+    def logits(x=x, out=x, **kw):
+        return _status(lpp.lpp_adjust_logits, tree, lpp.LPP_F32, x, 40, 0, 40, B, out, **kw)
+
+    one = torch.zeros(B)
+    assert logits(tokens=torch.zeros(B, M, **i32), repetition=one, bias=torch.zeros(40), mask=torch.zeros(B, M, 2, **i32)) == EHIP
+    assert logits(bias=torch.zeros(B, 40), mask=torch.zeros(B, 2, **i32)) == EHIP
+    for bad in (dict(x=x[:, :2]), dict(out=x.bfloat16()), dict(tokens=torch.zeros(B, M)), dict(counts=torch.zeros(B, 39, **i32)),
+                dict(repetition=one[:1]), dict(bias=torch.zeros(39)), dict(mask=torch.zeros(B, M, 1, **i32))):
+        assert logits(**bad) == EINVAL, bad
