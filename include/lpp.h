@@ -402,6 +402,38 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
                             const int32_t* page_table, int32_t table_stride, const int32_t* seq_len, int32_t B,
                             int32_t M, void* k_pages, void* v_pages, int32_t* new_len, void* stream);
 
+/* Attention of new tokens over the pages: out[b,h,i,:] = softmax_j(scale * <q[b,h,i], K_j>) V_j over the item's cached positions
+ * [0, seq_len[b]) and, of the new rows t,
+ *   lpp_paged_tree_attention    those with t == i or t an ancestor of i (the tree's M rows; a tree of the root alone is the
+ *                               decode step of one token)
+ *   lpp_paged_chunk_attention   those with t <= i: causal chunks of row_len[b] rows.  Rows of out behind an item's last are not
+ *                               written, rows of k_new and v_new behind it not used
+ * New rows are not read from the pages: commit or append them before or after.
+ *   q [B, H, M, Dh], k_tree / k_new and v_tree / v_new [B, Hkv, M, Dh], out [B, H, M, Dh]   [device] contiguous, of the cache's type,
+ *             16-byte aligned; Hkv divides H, query head h reads key/value head h / (H / Hkv)
+ *   S         [host] no item has more cached positions (seq_len is clamped to it); decides how the launch is cut, so that a bound far
+ *             above the lengths costs time.  S = 0: nothing is cached, pages and table may be NULL.  table_stride * page_size >= S
+ *   seq_len   [device] int32 [B] or NULL (= S);  row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M)
+ *   scale     0 selects 1/sqrt(Dh); negative, infinite or NaN is LPP_EINVAL
+ *   ws        lpp_paged_attention_workspace(cache, B, H, M, S) bytes
+ * Softmax and accumulation are float32; bf16 products run on the bf16 matrix cores with the weights rounded to bf16.  What a row
+ * does not see plays no part in it, whatever it holds.  Results do not depend on what is in ws or in pages beyond the lengths, and two
+ * calls with the same arguments give the same bits.
+ * Errors: LPP_EINVAL (null, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
+ * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, 2^31 blocks), LPP_ENOWORKSPACE,
+ * LPP_EHIP.
+ */
+size_t  lpp_paged_attention_workspace(const lpp_paged* cache, int32_t B, int32_t H, int32_t M, int32_t S);
+int32_t lpp_paged_tree_attention(const lpp_paged* cache, const lpp_tree* tree, const void* q, const void* k_pages,
+                                 const void* v_pages, const int32_t* page_table, int32_t table_stride,
+                                 const void* k_tree, const void* v_tree, const int32_t* seq_len, int32_t B, int32_t H,
+                                 int32_t S, float scale, void* out, void* ws, size_t ws_bytes, void* stream);
+int32_t lpp_paged_chunk_attention(const lpp_paged* cache, const void* q, const void* k_pages, const void* v_pages,
+                                  const int32_t* page_table, int32_t table_stride, const void* k_new,
+                                  const void* v_new, const int32_t* seq_len, const int32_t* row_len, int32_t B,
+                                  int32_t H, int32_t M, int32_t S, float scale, void* out, void* ws, size_t ws_bytes,
+                                  void* stream);
+
 /* -------------------------------------------------------- rotary positions ---
  * Between a layer's projections and its attention: queries and keys of a step's rows are turned by their positions,
  * values go along, and all three come out in the layouts that attention and commit read.

@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     LPP_BOUND_MULTIPLICATIVE, LPP_BOUND_ADDITIVE, LPP_RULE_PREFIX, LPP_RULE_SKIP,
     LPP_SIBLINGS_IID, LPP_SIBLINGS_DISTINCT,
     PagedCache, lpp_paged_commit_kv, lpp_paged_append_kv,
+    lpp_paged_tree_attention, lpp_paged_chunk_attention, lpp_paged_attention_workspace,
     Rotary, lpp_rotary_qkv, LPP_ROTARY_HALF, LPP_ROTARY_INTERLEAVED,
     LPP_ROTARY_NONE, LPP_ROTARY_LINEAR, LPP_ROTARY_NTK, LPP_ROTARY_YARN,
     lpp_adjust_logits, lpp_token_counts, lpp_commit_counts,

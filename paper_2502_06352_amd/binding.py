@@ -90,6 +90,12 @@ def lib() -> C.CDLL:
     L.lpp_paged_commit_kv.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp]
     L.lpp_paged_append_kv.restype = i32
     L.lpp_paged_append_kv.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp]
+    L.lpp_paged_attention_workspace.restype = sz
+    L.lpp_paged_attention_workspace.argtypes = [vp, i32, i32, i32, i32]
+    L.lpp_paged_tree_attention.restype = i32
+    L.lpp_paged_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, f32, vp, vp, sz, vp]
+    L.lpp_paged_chunk_attention.restype = i32
+    L.lpp_paged_chunk_attention.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, sz, vp]
     L.lpp_rotary_create.restype = i32; L.lpp_rotary_create.argtypes = [vp, C.POINTER(vp)]
     L.lpp_rotary_destroy.restype = i32; L.lpp_rotary_destroy.argtypes = [vp]
     L.lpp_rotary_qkv.restype = i32
@@ -403,6 +409,40 @@ def lpp_paged_append_kv(cache: PagedCache, k_new, v_new, row_len, page_table, se
         _maybe(w, "row_len", row_len, "i32", B, d), _table(w, page_table, B, d), page_table.shape[1],
         _want(w, "seq_len", seq_len, "i32", B, d), B, M, _want(w, "k_pages", k_pages, t, cache.pool, d),
         _want(w, "v_pages", v_pages, t, cache.pool, d), _maybe(w, "new_len", new_len, "i32", B, d), _on(stream, d)), w)
+
+
+def lpp_paged_attention_workspace(cache: PagedCache, B: int, H: int, M: int, S: int) -> int:
+    return int(lib().lpp_paged_attention_workspace(cache.handle, B, H, M, S))
+
+
+def _pages(where: str, cache: PagedCache, k_pages, v_pages, page_table, B: int, S: int, device: int):
+    if S == 0 and page_table is None:
+        return None, None, None, 0
+    return (_want(where, "k_pages", k_pages, cache.dtype, cache.pool, device),
+            _want(where, "v_pages", v_pages, cache.dtype, cache.pool, device), _table(where, page_table, B, device),
+            page_table.shape[1])
+
+
+def lpp_paged_tree_attention(cache: PagedCache, tree: Tree, q, k_pages, v_pages, page_table, k_tree, v_tree, seq_len, B: int,
+                             H: int, S: int, scale: float, out, ws, stream=None) -> None:
+    w, d, t, M = "lpp_paged_tree_attention", _device(), cache.dtype, tree.M
+    n, nkv = B * H * M * cache.Dh, B * cache.Hkv * M * cache.Dh
+    _check(lib().lpp_paged_tree_attention(
+        cache.handle, tree.handle, _want(w, "q", q, t, n, d), *_pages(w, cache, k_pages, v_pages, page_table, B, S, d),
+        _want(w, "k_tree", k_tree, t, nkv, d), _want(w, "v_tree", v_tree, t, nkv, d),
+        _maybe(w, "seq_len", seq_len, "i32", B, d), B, H, S, scale, _want(w, "out", out, t, n, d), _ptr(ws), _bytes(ws),
+        _on(stream, d)), w)
+
+
+def lpp_paged_chunk_attention(cache: PagedCache, q, k_pages, v_pages, page_table, k_new, v_new, seq_len, row_len, B: int,
+                              H: int, M: int, S: int, scale: float, out, ws, stream=None) -> None:
+    w, d, t = "lpp_paged_chunk_attention", _device(), cache.dtype
+    n, nkv = B * H * M * cache.Dh, B * cache.Hkv * M * cache.Dh
+    _check(lib().lpp_paged_chunk_attention(
+        cache.handle, _want(w, "q", q, t, n, d), *_pages(w, cache, k_pages, v_pages, page_table, B, S, d),
+        _want(w, "k_new", k_new, t, nkv, d), _want(w, "v_new", v_new, t, nkv, d),
+        _maybe(w, "seq_len", seq_len, "i32", B, d), _maybe(w, "row_len", row_len, "i32", B, d), B, H, M, S, scale,
+        _want(w, "out", out, t, n, d), _ptr(ws), _bytes(ws), _on(stream, d)), w)
 
 
 LPP_ROTARY_HALF, LPP_ROTARY_INTERLEAVED = 0, 1

@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblpp.so")
 SOURCES = ["lpp_tree.hip", "lpp_verify.hip", "lpp_attention.hip", "lpp_knn.hip", "lpp_commit.hip", "lpp_probe.hip",
-           "lpp_paged.hip", "lpp_rotary.hip", "lpp_logits.hip"]
+           "lpp_paged.hip", "lpp_paged_attention.hip", "lpp_rotary.hip", "lpp_logits.hip"]
 FLAGS = ["-O3", "-ffp-contract=off", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # matrix results in vector registers: every kernel here works on them right away, and out of the

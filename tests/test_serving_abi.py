@@ -69,6 +69,37 @@ def test_paged_writes_refuse(L):
     _refusals(append, {}, shared + [(dict(M=0), EINVAL), (dict(M=0x7FFFFFFF), EUNSUP), (dict(rows=FAKE), EHIP)])
 
 
+@no_gpu
+def test_paged_attention_refuses(L):
+    cache, tree = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0])
+
+    def trees(c=cache.handle, t=tree.handle, q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, stride=3, kn=FAKE, vn=FAKE, seq=None, B=2, H=4, S=40,
+              scale=0.0, out=FAKE, ws=FAKE, n=1 << 30):
+        return L.lpp_paged_tree_attention(c, t, q, kp, vp, table, stride, kn, vn, seq, B, H, S, scale, out, ws, n, None)
+
+    shared = [({}, EHIP), (dict(seq=FAKE), EHIP), (dict(c=None), EINVAL), (dict(q=None), EINVAL), (dict(kp=None), EINVAL), (dict(vp=None), EINVAL),
+              (dict(table=None), EINVAL), (dict(stride=0), EINVAL), (dict(stride=2), EINVAL), (dict(kn=None), EINVAL), (dict(vn=None), EINVAL),
+              (dict(B=0), EINVAL), (dict(H=0), EINVAL), (dict(H=3), EINVAL), (dict(S=-1), EINVAL), (dict(S=49), EINVAL),
+              (dict(S=0, kp=None, vp=None, table=None, stride=0), EHIP), (dict(scale=-1.0), EINVAL), (dict(scale=math.nan), EINVAL),
+              (dict(scale=math.inf), EINVAL), (dict(out=None), EINVAL), (dict(q=FAKE + 4), EINVAL), (dict(out=FAKE + 8), EINVAL),
+              (dict(kp=FAKE + 2), EINVAL), (dict(B=1 << 24), EUNSUP), (dict(S=1 << 30, stride=1 << 26), EUNSUP)]
+    _refusals(trees, {}, shared + [(dict(t=None), EINVAL)])
+    need = L.lpp_paged_attention_workspace(cache.handle, 1, 4, 3, 4000)
+    assert need > 256
+    for ws, n in ((None, need), (FAKE, need - 1), (FAKE + 4, need)):
+        assert trees(B=1, S=4000, stride=250, ws=ws, n=n) == lpp.LPP_ENOWORKSPACE
+    assert trees(B=1, S=4000, stride=250, n=need) == EHIP
+
+    def chunks(c=cache.handle, q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, stride=3, kn=FAKE, vn=FAKE, seq=None, rows=None, B=2, H=4, M=9, S=40,
+               scale=0.0, out=FAKE, ws=FAKE, n=1 << 30):
+        return L.lpp_paged_chunk_attention(c, q, kp, vp, table, stride, kn, vn, seq, rows, B, H, M, S, scale, out, ws, n, None)
+
+    _refusals(chunks, {}, shared + [(dict(rows=FAKE), EHIP), (dict(M=0), EINVAL), (dict(M=1 << 24), EUNSUP)])
+    assert L.lpp_paged_attention_workspace(None, 1, 4, 3, 40) == 0
+    for args in ((0, 4, 3, 40), (1, 3, 3, 40), (1, 4, 0, 40), (1, 4, 3, -1)):
+        assert L.lpp_paged_attention_workspace(cache.handle, *args) == 0
+
+
 def test_rotary_handle(L):
     def create(**kw):
         c = lpp.binding.RotaryConfig(**dict(dict(dim=64), **kw))
