@@ -50,6 +50,7 @@ struct PagedAttnArgs {
   float* ws_ml;                      // [item, head, row block][nsplit][ROWS][2]  reference maximum and sum
   uint32_t ws_o_bytes, ws_ml_bytes;
   int32_t* counters;                 // [item, head, row block] zero between calls
+  int32_t join_later;                // ranges are joined by a kernel of their own
 };
 
 // What a block works on.  The row blocks of a (item, head, range) read the same keys and sit on one XCD (block index mod 8) one
@@ -80,12 +81,12 @@ struct Cell {
   }
 };
 
-__device__ __forceinline__ int page_of(const PagedAttnArgs& a, int b, int pos, int seq) {
-  // (scalar loads, whatever is written meanwhile; positions past the last: its page again)
-  typedef const __attribute__((address_space(4))) int32_t* table_t;
-  const int page = ((table_t)(uintptr_t)a.table)[(int64_t)b * a.table_stride + (min(pos, seq - 1) >> a.page_shift)];
-  return min(max(page, 0), a.n_pages - 1);
+// Table entry of a position (past the last: of the last), and the page it names.
+__device__ __forceinline__ int entry_of(const PagedAttnArgs& a, int b, int pos, int seq) {
+  typedef const __attribute__((address_space(4))) int32_t* table_t;      // scalar loads, whatever is written meanwhile
+  return ((table_t)(uintptr_t)a.table)[(int64_t)b * a.table_stride + (min(pos, seq - 1) >> a.page_shift)];
 }
+__device__ __forceinline__ int page_of(const PagedAttnArgs& a, int entry) { return min(max(entry, 0), a.n_pages - 1); }
 
 // Whether row i sees new key t, 32 of them from t0 on (t0 a multiple of 32).
 __device__ __forceinline__ uint32_t sees32(const PagedAttnArgs& a, int row, int t0) {
@@ -123,11 +124,14 @@ __device__ __forceinline__ int64_t row_at(const PagedAttnArgs& a, int kvbh, int 
   return (((int64_t)kvbh * a.gq + (r - i * a.gq)) * a.M + i) * DH;
 }
 
-// The parts of a row tile's key ranges, added up in their order by the block that finishes last (`weight` of a difference of
-// references, at most 0): every wave waits until its own stores have completed, the barrier gathers the waves, then
+// What a part is multiplied by whose reference lies t below (at most 0): references are in units of log 2 for bf16.
+template <bool BF16>
+__device__ __forceinline__ float part_weight(float t) { return BF16 ? __builtin_amdgcn_exp2f(t) : exp_neg(t); }
+
+// The parts of a row tile's key ranges, added up in their order by the block that finishes last: every wave waits until its own stores have completed, the barrier gathers the waves, then
 // the ticket is taken; stores, ticket and loads are device-scope, so no cache is written back.
-template <int DH, int ROWS, int THREADS, bool BF16, typename W>
-__device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& c, int r0, int R, int ns, W weight) {
+template <int DH, int ROWS, int THREADS, bool BF16>
+__device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& c, int r0, int R, int ns) {
   __shared__ int s_ticket;
   const int tile = c.kvbh * a.row_blocks + c.rb;
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
@@ -158,13 +162,13 @@ __device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& 
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (s0 + u < ns) nm = fmaxf(nm, ml[u].x);
-      const float keep = weight(mm - nm);
+      const float keep = part_weight<BF16>(mm - nm);
       acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep; ll *= keep;
       mm = nm;
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (s0 + u < ns) {
-          const float f = weight(ml[u].x - mm);
+          const float f = part_weight<BF16>(ml[u].x - mm);
           ll += f * ml[u].y;
           acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
         }
@@ -178,6 +182,75 @@ __device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& 
     __hip_atomic_store(&a.counters[tile], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// The same for parts that are many, in a launch of its own: a lane has four numbers of a share of a row's ranges, shares are added in
+// their order.
+template <int DH, int ROWS, int SHARES, bool BF16>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int tiles_of_keys) {
+  constexpr int C4 = DH / 4, RPB = 256 / (C4 * SHARES), BPT = ROWS / RPB;    // rows of a block, blocks of a row tile
+  __shared__ __align__(16) float4 s_o[RPB][SHARES][C4];
+  __shared__ float s_m[RPB][SHARES], s_l[RPB][SHARES];
+  const int mine = threadIdx.x / (C4 * SHARES);
+  const int tile = (int)(blockIdx.x / BPT), r = (int)(blockIdx.x % BPT) * RPB + mine;
+  const int kvbh = tile / a.row_blocks, rb = tile - kvbh * a.row_blocks, b = kvbh / a.Hkv, r0 = rb * ROWS;
+  const int rows = a.row_len ? min(max(a.row_len[b], 0), a.M) : a.M, R = rows * a.gq;
+  if (r0 + r - mine >= R) return;
+  const int seq = a.seq_len ? min(max(a.seq_len[b], 0), a.S) : a.S;
+  const int fresh = (int)div_or_rc((uint32_t)(min(r0 + ROWS, R) - 1), (uint32_t)a.gq, a.rc_gq) + 1;
+  const int T = (seq + tiles_of_keys - 1) / tiles_of_keys + (fresh + tiles_of_keys - 1) / tiles_of_keys;
+  const int ns = (T + a.range - 1) / a.range;
+  if (ns == 1) return;                               // (the block wrote its rows itself)
+  const int c4 = threadIdx.x % C4, share = threadIdx.x / C4 % SHARES;
+  const int64_t part0 = (int64_t)tile * a.nsplit * ROWS + min(r, R - 1 - r0);
+  const float4* po = reinterpret_cast<const float4*>(a.ws_o);
+  const float2* pm = reinterpret_cast<const float2*>(a.ws_ml);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float ll = 0.f, mm = kMasked;
+  for (int s0 = share; s0 < ns; s0 += 4 * SHARES) {
+    float2 ml[4];
+    float4 o[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t prow = part0 + (int64_t)min(s0 + u * SHARES, ns - 1) * ROWS;
+      ml[u] = pm[prow];
+      o[u] = po[prow * C4 + c4];
+    }
+    float nm = mm;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u * SHARES < ns) nm = fmaxf(nm, ml[u].x);
+    const float keep = part_weight<BF16>(mm - nm);
+    acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep; ll *= keep;
+    mm = nm;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u * SHARES < ns) {
+        const float f = part_weight<BF16>(ml[u].x - mm);
+        ll += f * ml[u].y;
+        acc.x += f * o[u].x; acc.y += f * o[u].y; acc.z += f * o[u].z; acc.w += f * o[u].w;
+      }
+  }
+  s_o[mine][share][c4] = acc;
+  if (c4 == 0) { s_m[mine][share] = mm; s_l[mine][share] = ll; }
+  __syncthreads();
+  if (share > 0 || r0 + r >= R) return;
+  float top = kMasked;
+#pragma unroll
+  for (int w = 0; w < SHARES; ++w) top = fmaxf(top, s_m[mine][w]);
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  ll = 0.f;
+#pragma unroll
+  for (int w = 0; w < SHARES; ++w) {
+    const float f = part_weight<BF16>(s_m[mine][w] - top);
+    const float4 o = s_o[mine][w][c4];
+    ll += f * s_l[mine][w];
+    acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
+  }
+  const float inv = 1.0f / ll;
+  int m;
+  const int64_t e = row_at<DH>(a, kvbh, r0 + r, &m) + c4 * 4;
+  store_row4(a.out, BF16, e, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+}
+
 // ---------------------------------------------------------------- bf16
 
 // 64 pieces of 16 bytes from memory to LDS: piece `lane` from rsrc's base + off to lds + 16 lane.
@@ -186,6 +259,7 @@ __device__ __forceinline__ void to_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
   // compiler does not look inside)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
 }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }   // reads and writes of LDS are done
 template <int N>
 __device__ __forceinline__ void wait_loads() {      // until at most N of this wave's are in flight
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -199,25 +273,27 @@ __device__ __forceinline__ u32x4 buffer_at(uint64_t base) {
 // the banks evenly.
 template <int DH>
 __device__ __forceinline__ constexpr int swizzle(int row) {
-  return DH == 64 ? ((row >> 1 & 1) << 2) | ((row >> 2 & 1) << 1) | (row >> 3 & 1) : ((row & 7) << 1) | (row >> 3 & 1);
+  return DH == 64 ? ((row >> 1 & 1) << 2) | ((row >> 2 & 1) << 1) | (row >> 3 & 1) : ((row & 3) << 2) | (row >> 2 & 3);
 }
 
-// NT tiles of 32 rows a wave, WR waves along the rows (they share the tiles of keys), WK along the keys (each has its own tiles).
-template <int DH, int NT, int WR, int WK, int KT>
+// 32 rows a wave, WR waves along the rows (they share the tiles of keys), WK along the keys (each has its own tiles), ST places for a
+// tile.
+template <int DH, int WR, int WK, int KT, int ST>
 __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttnArgs a) {
-  static_assert(WR == 1 || WK == 1, "barriers inside the loop over the keys");
-  constexpr int W = WR * WK, ROWS = NT * WR * 32;
+  constexpr int W = WR * WK, ROWS = WR * 32;
   constexpr int KS = DH / 16, DT = DH / 32, SUB = KT / 32;
   constexpr int CPR = DH / 8;                        // pieces of a row
   constexpr int PITCH = DH * 2;
   constexpr int TILE = KT * PITCH;                   // bytes of K, and of V, of a tile
   constexpr int RPI = 64 / CPR;                      // rows of a load
   constexpr int NI = TILE / 1024 / WR;               // loads of K, and of V, of a tile and wave
-  constexpr int GROUPS = NI * RPI / 16;              // ... in groups of 16 rows: a page each at least
-  static_assert(GROUPS >= 1 && NI * RPI % 16 == 0, "a wave loads whole groups of 16 rows");
+  constexpr int RG = NI * RPI < 16 ? NI * RPI : 16;  // ... in groups of so many rows: of one page
+  constexpr int GROUPS = NI * RPI / RG;
+  static_assert(WR > 1 || KT == 32, "a wave by itself takes a tile at once");
+  static_assert(NI >= 1 && NI * RPI % RG == 0 && 16 % RG == 0, "whole groups of rows, none over a page's end");
   constexpr int OPITCH = DH + 4;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float s_m[W][NT * 32], s_l[W][NT * 32];
+  __shared__ float s_m[WK][ROWS], s_l[WK][ROWS];
   __shared__ int s_odd;
 
   const Cell c(a);
@@ -225,7 +301,7 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   if (r0 >= R) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
-  const int wr = WR > 1 ? wave : 0, kw = WK > 1 ? wave : 0;
+  const int wr = wave % WR, kw = wave / WR;
   const int m_first = (int)div_or_rc((uint32_t)r0, (uint32_t)a.gq, a.rc_gq);
   const int m_last = (int)div_or_rc((uint32_t)(min(r0 + ROWS, R) - 1), (uint32_t)a.gq, a.rc_gq);
   const int fresh = m_last + 1;                      // new keys that the block's rows can see: [0, fresh) (a tree's ancestors come first)
@@ -237,14 +313,13 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   if (threadIdx.x == 0) s_odd = 0;
 
   // Q as the B operand: column = row, 8 consecutive Dh a lane and step
-  bf16x8 qb[NT][KS];
-  int mrow[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int64_t e = row_at<DH>(a, c.kvbh, min(r0 + (wr * NT + nt) * 32 + l32, R - 1), &mrow[nt]);
+  bf16x8 qb[KS];
+  int mrow;
+  {
+    const int64_t e = row_at<DH>(a, c.kvbh, min(r0 + wr * 32 + l32, R - 1), &mrow);
     const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q) + e + half * 8;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qb[nt][ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
+    for (int ks = 0; ks < KS; ++ks) qb[ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
   }
 
   // loads: my piece of a group's rows; the row's part of the swizzle that a load's number decides comes on top
@@ -253,49 +328,42 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   const uint32_t loff = (uint32_t)(((lane % CPR) ^ swizzle<DH>(lrow)) * 16);
   const uint64_t page_bytes = (uint64_t)PITCH << a.page_shift;
   const uint64_t kn = (uint64_t)(uintptr_t)a.kn + (uint64_t)c.kvbh * a.M * PITCH, vn = (uint64_t)(uintptr_t)a.vn + (uint64_t)c.kvbh * a.M * PITCH;
-  int page[GROUPS];                                  // of the next tile to load
-  auto look_up = [&](int tile) {
+  int entry[GROUPS], ahead[GROUPS];                  // table entries of the next tile to load, and of the one behind it
+  auto look_up = [&](int (&e)[GROUPS], int tile) {
     if (tile >= TC || tile >= tend) return;
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) page[g] = page_of(a, c.b, tile * KT + (wr * GROUPS + g) * 16, seq);
+    for (int g = 0; g < GROUPS; ++g) e[g] = entry_of(a, c.b, tile * KT + (wr * GROUPS + g) * RG, seq);
   };
-  auto load_tile = [&](int tile, int stage) {
+  auto load_tile = [&](int tile, int stage, bool keys, bool values) {
     const uint32_t dst = lds0 + (uint32_t)((stage * WK + kw) * 2 * TILE + wr * NI * 1024);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int row0 = (wr * GROUPS + g) * 16;       // inside the tile
-      u32x4 kr, vr;
+      const int row0 = (wr * GROUPS + g) * RG;       // inside the tile
+      uint64_t k0 = kn, v0 = vn;
       if (tile < TC) {
-        const uint64_t at = ((uint64_t)page[g] * a.Hkv + c.kvh) * page_bytes +
+        const uint64_t at = ((uint64_t)page_of(a, entry[g]) * a.Hkv + c.kvh) * page_bytes +
                             (uint64_t)(((tile * KT + row0) & ((1 << a.page_shift) - 1)) * PITCH);
-        kr = buffer_at((uint64_t)(uintptr_t)a.kp + at);
-        vr = buffer_at((uint64_t)(uintptr_t)a.vp + at);
-      } else {
-        kr = buffer_at(kn);
-        vr = buffer_at(vn);
+        k0 = (uint64_t)(uintptr_t)a.kp + at;
+        v0 = (uint64_t)(uintptr_t)a.vp + at;
       }
+      const u32x4 kr = buffer_at(k0), vr = buffer_at(v0);
 #pragma unroll
-      for (int i = 0; i < 16 / RPI; ++i) {
-        const uint32_t piece = loff ^ (uint32_t)(swizzle<DH>(i * RPI) * 16);
+      for (int i = 0; i < RG / RPI; ++i) {
+        const uint32_t piece = loff ^ (uint32_t)(swizzle<DH>((RG < 16 ? row0 & 15 : 0) + i * RPI) * 16);
         const uint32_t off = piece + (uint32_t)((tile < TC ? i * RPI + lrow : min((tile - TC) * KT + row0 + i * RPI + lrow, a.M - 1)) * PITCH);
-        const uint32_t to = dst + (uint32_t)((g * (16 / RPI) + i) * 1024);
-        to_lds(kr, off, to);
-        to_lds(vr, off, to + TILE);
+        const uint32_t to = dst + (uint32_t)((g * (RG / RPI) + i) * 1024);
+        if (keys) to_lds(kr, off, to);
+        if (values) to_lds(vr, off, to + TILE);
       }
     }
   };
 
-  f32x16 oacc[NT][DT];
-  float m_ref[NT], l_sum[NT];
+  f32x16 oacc[DT];
+  float m_ref = kMasked, l_sum = 0.f;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m_ref[nt] = kMasked;
-    l_sum[nt] = 0.f;
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[nt][dt][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
   // where I read K: my row, piece 2 ks + half; and V: four numbers of the row that the transposing read wants of me
   const uint32_t kread = (uint32_t)(l32 * PITCH + ((half ^ swizzle<DH>(l32)) * 16));
   const int vrow = 4 * half + (l16 >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1);
@@ -303,100 +371,83 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
   bool odd = false;
 
-  auto work = [&](int tile, const unsigned char* base, auto full_tag) {
-    constexpr bool FULL = decltype(full_tag)::value;
-    const bool is_new = tile >= TC;
-    const int key0 = (is_new ? tile - TC : tile) * KT, limit = is_new ? fresh : seq;
+  auto scores = [&](const unsigned char* base, int kt) {
+    f32x16 s;
 #pragma unroll
-    for (int kt = 0; kt < SUB; ++kt) {
-      f32x16 s[NT];
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    bf16x8 ka[KS];                                   // (all asked for before the first product: left to the compiler, two at a time)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = *reinterpret_cast<const bf16x8*>(base + kt * 32 * PITCH + (kread ^ (uint32_t)(ks * 32)));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[nt][r] = 0.f;
+    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qb[ks], s, 0, 0, 0);
+    return s;
+  };
+  // Weights of 32 keys: I hold keys 8 (r / 4) + 4 half + r % 4 of column l32.  (One copy of this code for whole tiles and others: with
+  // two, the accumulators were moved from one's registers to the other's, 396 us instead of 378 for two chunks of 2048 rows.)
+  auto weights = [&](int tile, int kt, bool full, f32x16 s, bf16x8 (&pb)[2]) {
+    if (!full) {
+      const bool is_new = tile >= TC;
+      const int key0 = (is_new ? tile - TC : tile) * KT + kt * 32, left = (is_new ? fresh : seq) - key0;
+      uint32_t bits = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
+      if (is_new && left > 0) bits &= sees32(a, mrow, key0);
+      bits >>= 4 * half;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 ka = *reinterpret_cast<const bf16x8*>(base + kt * 32 * PITCH + (kread ^ (uint32_t)(ks * 32)));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[nt][ks], s[nt], 0, 0, 0);
-      }
-      // weights: I hold keys 8 (r / 4) + 4 half + r % 4 of column l32
-      uint32_t bits[NT];
-      float mx[NT];
-      bool need = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        bits[nt] = 0xFFFFFFFFu;
-        if (!FULL) {
-          const int left = limit - key0 - kt * 32;
-          bits[nt] = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
-          if (is_new && left > 0) bits[nt] &= sees32(a, mrow[nt], key0 + kt * 32);
-          bits[nt] >>= 4 * half;
-        }
-        float v = kMasked;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x = s[nt][r];
-          if (!FULL && !((bits[nt] >> (8 * (r >> 2) + (r & 3))) & 1u)) x = kMasked;
-          v = fmaxf(v, x);
-        }
-        mx[nt] = v > 0.5f * kMasked ? v * a.scale : kMasked;       // (scale > 0: the maximum commutes with it)
-        need = need || mx[nt] > m_ref[nt] + kLazy;
-      }
-      if (__ballot(need)) {                          // some row's reference moves: rare behind the first tile
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float v = fmaxf(mx[nt], __shfl_xor(mx[nt], 32));
-          const float nm = v > m_ref[nt] + kLazy ? v : m_ref[nt];
-          const float alpha = __builtin_amdgcn_exp2f(m_ref[nt] - nm);
-          m_ref[nt] = nm;
-          l_sum[nt] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) oacc[nt][dt] *= alpha;
-        }
-      }
-      bf16x8 pb[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        uint32_t pk[8];
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][r], a.scale, -m_ref[nt]));
-          float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][r + 1], a.scale, -m_ref[nt]));
-          if (!FULL) {
-            if (!((bits[nt] >> (8 * (r >> 2) + (r & 3))) & 1u)) p0 = 0.f;
-            if (!((bits[nt] >> (8 * (r >> 2) + (r & 3) + 1)) & 1u)) p1 = 0.f;
-          }
-          pk[r / 2] = pack_bf16(p0, p1);
-          l_sum[nt] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[r / 2]), ones, l_sum[nt], false);
-        }
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) pb[nt][s2] = __builtin_bit_cast(bf16x8, make_uint4(pk[4 * s2], pk[4 * s2 + 1], pk[4 * s2 + 2], pk[4 * s2 + 3]));
-      }
-      // contraction slot (half, j) of step s2 is key 16 s2 + (j < 4 ? 0 : 8) + 4 half + j % 4 on both sides
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const unsigned char* src = base + TILE + (kt * 32 + 16 * s2) * PITCH;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (s16x4 __attribute__((address_space(3)))*)(const __attribute__((address_space(3))) unsigned char*)(src + (vread ^ (uint32_t)(dt * 64))));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (s16x4 __attribute__((address_space(3)))*)(const __attribute__((address_space(3))) unsigned char*)(
-                  src + 8 * PITCH + (vread ^ (uint32_t)(dt * 64) ^ (uint32_t)(swizzle<DH>(8) * 16))));
-          const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-          const bf16x8 va = __builtin_bit_cast(bf16x8, make_uint4(l2.x, l2.y, h2.x, h2.y));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) oacc[nt][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[nt][s2], oacc[nt][dt], 0, 0, 0);
-        }
+      for (int r = 0; r < 16; ++r) s[r] = (bits >> (8 * (r >> 2) + (r & 3))) & 1u ? s[r] : -INFINITY;
     }
+    float mx = kMasked;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = mx > 0.5f * kMasked ? mx * a.scale : kMasked;               // (scale > 0: the maximum commutes with it)
+    if (__ballot(mx > m_ref + kLazy)) {              // some row's reference moves: rare behind the first tile
+      const float v = fmaxf(mx, __shfl_xor(mx, 32));
+      const float nm = v > m_ref + kLazy ? v : m_ref;
+      const float alpha = __builtin_amdgcn_exp2f(m_ref - nm);
+      m_ref = nm;
+      l_sum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+    }
+    uint32_t pk[8];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale, -m_ref));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], a.scale, -m_ref));
+      pk[r / 2] = pack_bf16(p0, p1);
+      l_sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[r / 2]), ones, l_sum, false);
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) pb[s2] = __builtin_bit_cast(bf16x8, make_uint4(pk[4 * s2], pk[4 * s2 + 1], pk[4 * s2 + 2], pk[4 * s2 + 3]));
+  };
+  auto read_values = [&](const unsigned char* base, int kt, bf16x8 (&va)[2][DT]) {
+    typedef s16x4 __attribute__((address_space(3))) * lds_t;
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const __attribute__((address_space(3))) unsigned char* src =
+            (const __attribute__((address_space(3))) unsigned char*)(base + TILE + (kt * 32 + 16 * s2) * PITCH);
+        const uint32_t at = vread ^ (uint32_t)(dt * 64);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(src + at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(src + 8 * PITCH + (at ^ (uint32_t)(swizzle<DH>(8) * 16))));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        va[s2][dt] = __builtin_bit_cast(bf16x8, make_uint4(l2.x, l2.y, h2.x, h2.y));
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto add_values = [&](const bf16x8 (&va)[2][DT], const bf16x8 (&pb)[2]) {
+    // contraction slot (half, j) of step s2 is key 16 s2 + (j < 4 ? 0 : 8) + 4 half + j % 4 on both sides
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[s2][dt], pb[s2], oacc[dt], 0, 0, 0);
   };
   // A tile with keys that are not there, or that some row does not see: values of the former become zeros (their slots may hold
   // anything), and so do infinities and NaN among new ones (see add_odd).
   auto clean = [&](int tile, unsigned char* values) {
     const bool is_new = tile >= TC;
     const int here = (is_new ? fresh - (tile - TC) * KT : seq - tile * KT);
-    for (int p = WR > 1 ? (int)threadIdx.x : lane; p < KT * CPR; p += WR * 64) {
+    for (int p = wr * 64 + lane; p < KT * CPR; p += WR * 64) {
       uint4* at = reinterpret_cast<uint4*>(values + p * 16);
       if (p / CPR >= here) {
         *at = make_uint4(0, 0, 0, 0);
@@ -411,46 +462,87 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
         if (found) { *at = make_uint4(w[0], w[1], w[2], w[3]); odd = true; }
       }
     }
-    if (WR > 1) __syncthreads();
-    else wave_lds_sync();
   };
+  // (only the last tile of the cache, where it is not whole, and new ones: all of a tree's, of a chunk's those that some row of the block is ahead of)
+  const int part_tile = seq % KT != 0 ? TC - 1 : T, masked0 = TC + (a.anc ? 0 : (m_first + 1) / KT);
+  auto is_full = [&](int tile) { return tile != part_tile && tile < masked0; };
 
   __syncthreads();                                   // (s_odd is cleared before any wave sets it)
   // Q has arrived before the first load to LDS is issued: a wait for it inside the loop would wait for those as well
-  look_up(tbeg + kw);
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int g = 0; g < GROUPS; ++g) entry[g] = ahead[g] = 0;
+  look_up(entry, tbeg + kw);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qb[nt][ks]));
-  if (tbeg + kw < tend) load_tile(tbeg + kw, 0);
-  look_up(tbeg + kw + WK);
-  int stage = 0;
-  for (int tile = tbeg + kw; tile < tend; tile += WK) {
-    const bool more = tile + WK < tend;
-    if (WR > 1) {
-      wait_loads<0>();
-      __syncthreads();                               // the tile is there, and everybody is done with the one before it
-      if (more) load_tile(tile + WK, stage ^ 1);
-    } else if (more) {
-      __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): what was read of that stage has been read
-      load_tile(tile + WK, stage ^ 1);
-      wait_loads<2 * NI>();
-    } else {
-      wait_loads<0>();
-    }
-    if (more) look_up(tile + 2 * WK);
-    unsigned char* base = smem + (stage * WK + kw) * 2 * TILE;
-    const bool full = tile < TC ? (tile + 1) * KT <= seq : !a.anc && (tile - TC + 1) * KT <= m_first + 1;
-    if (full) {
-      work(tile, base, std::integral_constant<bool, true>());
-    } else {
-      clean(tile, base + TILE);
-      work(tile, base, std::integral_constant<bool, false>());
-    }
-    stage ^= 1;
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qb[ks]));
+  if (tbeg + kw < tend) {                            // (the keys' loads first: they are waited for by their number)
+    load_tile(tbeg + kw, 0, true, false);
+    load_tile(tbeg + kw, 0, false, true);
   }
+  look_up(entry, tbeg + kw + WK);
+  if (WR == 1) {
+    // A wave by itself, one place for its tile: the next tile's keys go where this one's were as soon as the scores are formed, the values
+    // likewise.  (Two places would halve the waves that a compute unit holds; one wave waits where another works.)
+    unsigned char* base = smem + kw * 2 * TILE;
+    for (int tile = tbeg + kw; tile < tend; tile += WK) {
+      const bool more = tile + WK < tend, full = is_full(tile);
+      look_up(ahead, tile + 2 * WK);                 // (they arrive while the tile is waited for)
+      wait_loads<NI>();                              // the keys; the values may be on their way
+      bf16x8 pb[2], va[2][DT];
+      const f32x16 s = scores(base, 0);
+      wait_lds();
+      if (more) load_tile(tile + WK, 0, true, false);
+      weights(tile, 0, full, s, pb);
+      if (more) wait_loads<NI>();                    // the values
+      else wait_loads<0>();
+      if (!full) {
+        clean(tile, base + TILE);
+        wave_lds_sync();
+      }
+      read_values(base, 0, va);
+      add_values(va, pb);
+      wait_lds();
+      if (more) load_tile(tile + WK, 0, false, true);
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) l_sum[nt] += __shfl_xor(l_sum[nt], 32);
+      for (int g = 0; g < GROUPS; ++g) entry[g] = ahead[g];
+    }
+  } else {
+    int stage = 0;
+#pragma unroll
+    for (int d = 1; d < ST - 1; ++d) {
+      if (tbeg + kw + d * WK < tend) load_tile(tbeg + kw + d * WK, d, true, true);
+      look_up(entry, tbeg + kw + (d + 1) * WK);
+    }
+    for (int first = tbeg; first < tend; first += WK) { // (the same rounds for all waves: they meet in them)
+      const int tile = first + kw;
+      look_up(ahead, tile + ST * WK);
+      if (tile + (ST - 2) * WK < tend) wait_loads<(ST - 2) * 2 * NI>();
+      else wait_loads<0>();
+      __syncthreads();                               // the tile is there, and everybody is done with the one before it
+      if (tile + (ST - 1) * WK < tend) load_tile(tile + (ST - 1) * WK, (stage + ST - 1) % ST, true, true);
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) entry[g] = ahead[g];
+      unsigned char* base = smem + (stage * WK + kw) * 2 * TILE;
+      const int last = min(first + WK, tend) - 1;
+      const bool all_full = (part_tile < first || part_tile > last) && last < masked0;
+      const bool full = is_full(tile);
+      if (!all_full) {
+        if (tile < tend && !full) clean(tile, base + TILE);
+        __syncthreads();
+      }
+      if (tile < tend) {
+#pragma unroll
+        for (int kt = 0; kt < SUB; ++kt) {
+          bf16x8 pb[2], va[2][DT];
+          const f32x16 s = scores(base, kt);
+          read_values(base, kt, va);
+          weights(tile, kt, full, s, pb);
+          add_values(va, pb);
+        }
+      }
+      stage = stage + 1 == ST ? 0 : stage + 1;
+    }
+  }
+  l_sum += __shfl_xor(l_sum, 32);
   if (odd) s_odd = 1;
 
   const int new0 = max(tbeg - TC, 0) * KT, new1 = min(max(tend - TC, 0) * KT, fresh);    // new keys of this range
@@ -460,47 +552,39 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   if (WK == 1) {
     __syncthreads();
     const bool fix = s_odd != 0;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = (wr * NT + nt) * 32 + l32;
-      if (r0 + r >= R) continue;
+    const int r = wr * 32 + l32;
+    if (r0 + r < R) {
       int m;
       const int64_t e = row_at<DH>(a, c.kvbh, r0 + r, &m);
-      const float inv = ns == 1 ? 1.0f / l_sum[nt] : 1.0f;
+      const float inv = ns == 1 ? 1.0f / l_sum : 1.0f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int d = dt * 32 + g * 8 + half * 4;
-          float4 v = make_float4(oacc[nt][dt][4 * g] * inv, oacc[nt][dt][4 * g + 1] * inv, oacc[nt][dt][4 * g + 2] * inv, oacc[nt][dt][4 * g + 3] * inv);
+          float4 v = make_float4(oacc[dt][4 * g] * inv, oacc[dt][4 * g + 1] * inv, oacc[dt][4 * g + 2] * inv, oacc[dt][4 * g + 3] * inv);
           if (fix) add_odd(a, vnew, DH, m, d, new0, new1, v);
           if (ns == 1) store_row4(a.out, true, e + d, v);
           else store_dev(dev_o, ((part + r) * DH + d) * 4, v);
         }
-      if (ns > 1 && half == 0) store_dev(dev_ml, (part + r) * 8, make_float2(m_ref[nt], l_sum[nt]));
+      if (ns > 1 && half == 0) store_dev(dev_ml, (part + r) * 8, make_float2(m_ref, l_sum));
     }
   } else {
     // the waves' parts of the rows are added in their order
-    if (half == 0) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) { s_m[wave][nt * 32 + l32] = m_ref[nt]; s_l[wave][nt * 32 + l32] = l_sum[nt]; }
-    }
+    const int col = wr * 32 + l32;
+    if (half == 0) { s_m[kw][col] = m_ref; s_l[kw][col] = l_sum; }
     __syncthreads();                                 // every wave is done with its tiles too
-    float* s_o = reinterpret_cast<float*>(smem);     // [W][ROWS][OPITCH]
+    float* s_o = reinterpret_cast<float*>(smem);     // [WK][ROWS][OPITCH]
+    float top = kMasked;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int col = nt * 32 + l32;
-      float mm = kMasked;
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, s_m[w][col]);
+    const float f = __builtin_amdgcn_exp2f(m_ref - top);
 #pragma unroll
-      for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w][col]);
-      const float f = __builtin_amdgcn_exp2f(m_ref[nt] - mm);
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<float4*>(&s_o[(wave * ROWS + col) * OPITCH + dt * 32 + g * 8 + half * 4]) =
-              make_float4(oacc[nt][dt][4 * g] * f, oacc[nt][dt][4 * g + 1] * f, oacc[nt][dt][4 * g + 2] * f, oacc[nt][dt][4 * g + 3] * f);
-    }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(&s_o[(kw * ROWS + col) * OPITCH + dt * 32 + g * 8 + half * 4]) =
+            make_float4(oacc[dt][4 * g] * f, oacc[dt][4 * g + 1] * f, oacc[dt][4 * g + 2] * f, oacc[dt][4 * g + 3] * f);
     __syncthreads();
     const bool fix = s_odd != 0;
     constexpr int C4 = DH / 4;
@@ -509,10 +593,10 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
       if (r0 + r >= R) continue;
       float mm = kMasked, ll = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w][r]);
+      for (int w = 0; w < WK; ++w) mm = fmaxf(mm, s_m[w][r]);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
+      for (int w = 0; w < WK; ++w) {
         ll += __builtin_amdgcn_exp2f(s_m[w][r] - mm) * s_l[w][r];
         const float4 o = *reinterpret_cast<const float4*>(&s_o[(w * ROWS + r) * OPITCH + c4 * 4]);
         v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
@@ -529,20 +613,21 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
       }
     }
   }
-  if (ns == 1) return;
-  join_ranges<DH, ROWS, W * 64, true>(a, c, r0, R, ns, [](float t) { return __builtin_amdgcn_exp2f(t); });
+  if (ns == 1 || a.join_later) return;
+  join_ranges<DH, ROWS, W * 64, true>(a, c, r0, R, ns);
 }
 
 // ---------------------------------------------------------------- float32
 
-// A block is 16 rows; its W waves take the 16-key tiles of its range in turn.  Lane (i, g) of a wave holds of key i the dimensions 16 t + 4 g .. + 3, and of
-// keys 4 g + r the values of dimensions 64 h + 4 i .. + 3: what its 16-byte loads bring is what both products want.
-template <int DH, int W>
+// A block is NT tiles of 16 rows; its W waves take the 16-key tiles of its range in turn.  Lane (i, g) of a wave holds of key i the
+// dimensions 16 t + 4 g .. + 3, and of keys 4 g + r the values of dimensions 64 h + 4 i .. + 3: what its 16-byte loads bring is what both products
+// want.  Bound by what a compute unit takes in (every block reads all keys of its range): two tiles of rows share what is loaded.
+template <int DH, int NT, int W>
 __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a) {
-  constexpr int ROWS = 16, HT = DH / 64, P4 = DH / 4 + 1;
+  constexpr int ROWS = 16 * NT, HT = DH / 64, P4 = DH / 4 + 1;
   extern __shared__ __align__(16) unsigned char smem[];
-  float4* const s_o = reinterpret_cast<float4*>(smem);      // [W][16][P4]
-  __shared__ float s_m[W][16], s_l[W][16];
+  float4* const s_o = reinterpret_cast<float4*>(smem);      // [W][ROWS][P4]
+  __shared__ float s_m[W][ROWS], s_l[W][ROWS];
   __shared__ int s_odd;
   const Cell c(a);
   const int R = c.rows * a.gq, r0 = c.rb * ROWS;
@@ -554,17 +639,22 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
   if (c.split >= ns) return;
   const int tbeg = c.split * a.range, tend = min(tbeg + a.range, T);
   if (threadIdx.x == 0) s_odd = 0;
-  int row;
-  const float* qp = reinterpret_cast<const float*>(a.q) + row_at<DH>(a, c.kvbh, min(r0 + i, R - 1), &row);
-  f32x4 q[DH / 16], acc[4 * HT];
+  int row[NT];
+  f32x4 q[NT][DH / 16], acc[NT][4 * HT];
+  float m[NT], l[NT];
 #pragma unroll
-  for (int t = 0; t < DH / 16; ++t) q[t] = *reinterpret_cast<const f32x4*>(qp + 16 * t + 4 * g);
+  for (int nt = 0; nt < NT; ++nt) {
+    const float* qp = reinterpret_cast<const float*>(a.q) + row_at<DH>(a, c.kvbh, min(r0 + nt * 16 + i, R - 1), &row[nt]);
 #pragma unroll
-  for (int d = 0; d < 4 * HT; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < DH / 16; ++t) q[nt][t] = *reinterpret_cast<const f32x4*>(qp + 16 * t + 4 * g);
+#pragma unroll
+    for (int d = 0; d < 4 * HT; ++d) acc[nt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[nt] = kMasked;
+    l[nt] = 0.f;
+  }
   __syncthreads();                                   // (s_odd is cleared before any wave sets it)
   const int64_t page_size = (int64_t)DH << a.page_shift;
   const int64_t new_at = (int64_t)c.kvbh * a.M * DH;
-  float m = kMasked, l = 0.f;
   bool odd = false;
   for (int tile = tbeg + wave; tile < tend; tile += W) {
     const bool is_new = tile >= TC;
@@ -574,7 +664,7 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
       kp = reinterpret_cast<const float*>(a.kn) + new_at + (int64_t)key0 * DH;
       vp = reinterpret_cast<const float*>(a.vn) + new_at + (int64_t)key0 * DH;
     } else {
-      const int64_t at = ((int64_t)page_of(a, c.b, key0, seq) * a.Hkv + c.kvh) * page_size + (int64_t)(key0 & ((1 << a.page_shift) - 1)) * DH;
+      const int64_t at = ((int64_t)page_of(a, entry_of(a, c.b, key0, seq)) * a.Hkv + c.kvh) * page_size + (int64_t)(key0 & ((1 << a.page_shift) - 1)) * DH;
       kp = reinterpret_cast<const float*>(a.kp) + at;
       vp = reinterpret_cast<const float*>(a.vp) + at;
     }
@@ -586,73 +676,86 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int h = 0; h < HT; ++h) v[r][h] = *reinterpret_cast<const f32x4*>(vp + min(4 * g + r, last) * DH + 64 * h + 4 * i);
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};                    // chains of Dh / 4 products, two at a time
-#pragma unroll
-    for (int t0 = 0; t0 < DH / 16; t0 += DH / 32) {
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = t0; t < t0 + DH / 32; t += 2)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][e], q[t][e], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t + 1][e], q[t + 1][e], s1, 0, 0, 0);
-        }
-      s += s0 + s1;
-    }
-    uint32_t bits = limit - key0 >= 16 ? 0xFFFFu : (1u << (limit - key0)) - 1u;
-    if (is_new) {
-      bits &= sees32(a, row, key0 & ~31) >> (key0 & 31);
+    const uint32_t there = (limit - key0 >= 16 ? 0xFFFFu : (1u << (limit - key0)) - 1u) >> (4 * g);
+    if (is_new || last < 15) {                         // what is not there counts as zeros, and so do infinities and NaN among new values (see add_odd)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int h = 0; h < HT; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!isfinite(v[r][h][e])) { v[r][h][e] = 0.f; odd = true; }
+          for (int e = 0; e < 4; ++e) {
+            const bool here = (there >> r) & 1u, off = is_new && here && !isfinite(v[r][h][e]);
+            odd = odd || off;
+            v[r][h][e] = here && !off ? v[r][h][e] : 0.f;
+          }
     }
-    bits >>= 4 * g;
-    float mn = kMasked, sc[4];
+    float sc[NT][4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      sc[r] = (bits >> r) & 1u ? s[r] * a.scale : kMasked;
-      mn = fmaxf(mn, sc[r]);
+    for (int nt = 0; nt < NT; ++nt) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};                  // chains of Dh / 4 products, two at a time
+#pragma unroll
+      for (int t0 = 0; t0 < DH / 16; t0 += DH / 32) {
+        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = t0; t < t0 + DH / 32; t += 2)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][e], q[nt][t][e], s0, 0, 0, 0);
+            s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t + 1][e], q[nt][t + 1][e], s1, 0, 0, 0);
+          }
+        s += s0 + s1;
+      }
+      const uint32_t bits = is_new ? there & (sees32(a, row[nt], key0 & ~31) >> ((key0 & 31) + 4 * g)) : there;
+      float mn = kMasked;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[nt][r] = (bits >> r) & 1u ? s[r] * a.scale : -INFINITY;
+        mn = fmaxf(mn, sc[nt][r]);
+      }
+      mn = fmaxf(mn, __shfl_xor(mn, 16));
+      mn = fmaxf(mn, __shfl_xor(mn, 32));
+      mn = fmaxf(mn, m[nt]);
+      if (__any(mn != m[nt])) {
+        const float f = mn == m[nt] ? 1.f : exp_neg(m[nt] - mn);
+        l[nt] *= f;
+#pragma unroll
+        for (int d = 0; d < 4 * HT; ++d) acc[nt][d] *= f;
+        m[nt] = mn;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[nt][r] = sc[nt][r] == -INFINITY ? 0.f : exp_neg(sc[nt][r] - m[nt]);
+        l[nt] += sc[nt][r];
+      }
     }
-    mn = fmaxf(mn, __shfl_xor(mn, 16));
-    mn = fmaxf(mn, __shfl_xor(mn, 32));
-    mn = fmaxf(mn, m);
-    if (__any(mn != m)) {
-      const float f = mn == m ? 1.f : exp_neg(m - mn);
-      l *= f;
 #pragma unroll
-      for (int d = 0; d < 4 * HT; ++d) acc[d] *= f;
-      m = mn;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      sc[r] = (bits >> r) & 1u ? exp_neg(sc[r] - m) : 0.f;
-      l += sc[r];
-      const bool there = key0 + 4 * g + r < limit;      // (values that are not there: the last's, weight 0)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int h = 0; h < HT; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(there ? v[r][h][e] : 0.f, sc[r], acc[4 * h + e], 0, 0, 0);
-    }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            acc[nt][4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][h][e], sc[nt][r], acc[nt][4 * h + e], 0, 0, 0);
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (lane < 16) { s_m[wave][lane] = m; s_l[wave][lane] = l; }
   if (odd) s_odd = 1;
 #pragma unroll
-  for (int h = 0; h < HT; ++h)
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += __shfl_xor(l[nt], 16);
+    l[nt] += __shfl_xor(l[nt], 32);
+    if (lane < 16) { s_m[wave][nt * 16 + lane] = m[nt]; s_l[wave][nt * 16 + lane] = l[nt]; }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      s_o[(wave * 16 + i) * P4 + 16 * h + 4 * g + r] = make_float4(acc[4 * h][r], acc[4 * h + 1][r], acc[4 * h + 2][r], acc[4 * h + 3][r]);
+    for (int h = 0; h < HT; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        s_o[(wave * ROWS + nt * 16 + i) * P4 + 16 * h + 4 * g + r] =
+            make_float4(acc[nt][4 * h][r], acc[nt][4 * h + 1][r], acc[nt][4 * h + 2][r], acc[nt][4 * h + 3][r]);
+  }
   __syncthreads();
 
   const __amdgpu_buffer_rsrc_t dev_o = device_buffer(a.ws_o, a.ws_o_bytes), dev_ml = device_buffer(a.ws_ml, a.ws_ml_bytes);
   const uint32_t part = (uint32_t)((c.kvbh * a.row_blocks + c.rb) * a.nsplit + c.split) * ROWS;
-  for (int idx = threadIdx.x; idx < 16 * DH / 4; idx += W * 64) {
+  for (int idx = threadIdx.x; idx < ROWS * DH / 4; idx += W * 64) {
     const int r = idx / (DH / 4), c4 = idx % (DH / 4);
     if (r0 + r >= R) continue;
     float mm = kMasked, ll = 0.f;
@@ -662,7 +765,7 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float f = exp_neg(s_m[w][r] - mm);
-      const float4 x = s_o[(w * 16 + r) * P4 + c4];
+      const float4 x = s_o[(w * ROWS + r) * P4 + c4];
       ll = __builtin_fmaf(f, s_l[w][r], ll);
       o.x = __builtin_fmaf(f, x.x, o.x); o.y = __builtin_fmaf(f, x.y, o.y); o.z = __builtin_fmaf(f, x.z, o.z); o.w = __builtin_fmaf(f, x.w, o.w);
     }
@@ -679,49 +782,79 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
       if (c4 == 0) store_dev(dev_ml, (part + r) * 8, make_float2(mm, ll));
     }
   }
-  if (ns == 1) return;
-  join_ranges<DH, ROWS, W * 64, false>(a, c, r0, R, ns, [](float t) { return exp_neg(t); });
+  if (ns == 1 || a.join_later) return;
+  join_ranges<DH, ROWS, W * 64, false>(a, c, r0, R, ns);
 }
 
 // ---------------------------------------------------------------- host
 
 struct PagedPlan {
-  int nt, wr, wk, kt, rows;          // shape of a block
+  int shape, rows, kt, wk;           // bf16: which of kShapes; rows of a block, keys of a tile, waves along the keys
   int row_blocks, nsplit, range;
+  bool join_later;
   size_t lds;
   size_t o_bytes, ml_bytes;          // partials
 };
 
+// Shapes of a bf16 block, and what a round of its waves (kt * wk keys) costs in microseconds: with heads of 64 and of 128 numbers, the
+// block by itself on a compute unit and each of many there.  Measured: 28 shapes of input (1 to 384 heads in all, 4 to 8192 rows, 100
+// to 32768 keys) with 1 to 128 ranges of keys, 1 to 16 ranges joined in both ways; the constants are fitted to those times.
+struct Shape { int wr, wk, kt, st; int resident[2]; float alone[2], each[2]; };
+constexpr Shape kShapes[] = {
+    {1, 4, 32, 1, {4, 2}, {0.83f, 1.32f}, {0.37f, 1.10f}},
+    {1, 8, 32, 1, {2, 1}, {0.84f, 1.22f}, {0.79f, 1.86f}},
+    {2, 4, 32, 2, {2, 1}, {0.87f, 0.93f}, {0.62f, 1.41f}},
+    {4, 1, 64, 2, {3, 2}, {0.97f, 1.94f}, {0.60f, 0.50f}},
+    {4, 2, 32, 2, {2, 1}, {0.76f, 1.00f}, {0.62f, 1.10f}},
+};
+constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+
+// What adding up the ranges of a launch costs: by the block that finishes last (bytes: of a row tile) or in a launch of its own, which
+// reads with all compute units.  (1 head, 108 rows, 21419 keys in 32 ranges: 34 us and 19; 8 heads, 4 rows, 2400 keys in 6: 12.4 and 12.7.)
+inline float join_last(double bytes) { return 3.2f + (float)(bytes / 18900.); }
+inline float join_launch(double bytes) { return 3.4f + (float)(bytes / 1540000.); }
+
+// The shape and the number of ranges whose estimate is least: rounds of a block, each as long as a compute unit takes with the
+// blocks that fall to it, a fixed cost for every block there, and the joining.  Over the inputs above the choices take 1.02 times the best of
+// all measured ones; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8 times that.
 PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64_t S) {
-  PagedPlan p;
-  const int64_t R = M * gq;
-  const int Dh = cache->Dh;
-  int resident;                      // blocks that a compute unit holds
-  if (cache->dtype == LPP_F32) {
-    p.nt = 1; p.wr = 1; p.wk = Dh == 64 ? 16 : 8; p.kt = 16; p.rows = 16;
-    p.lds = (size_t)p.wk * 16 * (Dh + 4) * sizeof(float);
-    resident = 2;
-  } else {
-    if (R <= 32) { p.nt = 1; p.wr = 1; p.wk = 4; p.kt = 32; }
-    else if (R <= 64) { p.nt = 2; p.wr = 1; p.wk = 4; p.kt = 32; }
-    else { p.nt = 1; p.wr = 4; p.wk = 1; p.kt = 64; }
-    p.rows = p.nt * p.wr * 32;
-    const size_t tiles = (size_t)2 * p.wk * 2 * p.kt * Dh * 2;
-    const size_t merge = p.wk > 1 ? (size_t)p.wk * p.rows * (Dh + 4) * sizeof(float) : 0;
-    p.lds = std::max(tiles, merge);
-    resident = std::max<int>(1, std::min<int>(2, (int)(150 * 1024 / p.lds)));
+  PagedPlan p{};
+  const int64_t R = M * gq, heads = B * cache->Hkv;
+  const int Dh = cache->Dh, d = Dh == 128;
+  const bool bf16 = cache->dtype == LPP_BF16;
+  const Shape f32[2] = {{1, Dh == 64 ? 16 : 8, 16, 0, {1, 1}, {3.3f, 3.2f}, {3.1f, 3.2f}}, {2, 8, 16, 0, {1, 1}, {3.0f, 5.2f}, {2.9f, 5.5f}}};
+  double best = INFINITY;
+  for (int i = 0; i < (bf16 ? (int)(sizeof(kShapes) / sizeof(kShapes[0])) : 2); ++i) {
+    const Shape& h = bf16 ? kShapes[i] : f32[i];
+    const int rows = h.wr * (bf16 ? 32 : 16);
+    const int64_t row_blocks = (R + rows - 1) / rows, units = heads * row_blocks;
+    const int64_t tiles = (S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt, rounds = (tiles + h.wk - 1) / h.wk;
+    int64_t before = 0;
+    for (const int g : kRanges) {
+      const int64_t per = (rounds + std::min<int64_t>(g, rounds) - 1) / std::min<int64_t>(g, rounds), ranges = (rounds + per - 1) / per, blocks = units * ranges;
+      if (ranges == before) continue;                // (as many as the last choice)
+      before = ranges;
+      if (ranges > 1 && blocks * rows * (Dh + 2) * 4 >= (int64_t)1 << 31) break;      // (32-bit offsets into the parts)
+      const int64_t k = (blocks + cache->n_cu - 1) / cache->n_cu;
+      const double load = std::max(1., (double)blocks / cache->n_cu);
+      double t = (double)per * std::max<double>(h.alone[d] * (double)((k + h.resident[d] - 1) / h.resident[d]), h.each[d] * load) + 0.7 * (double)k;
+      bool later = false;
+      if (ranges > 1) {
+        const double bytes = (double)ranges * (double)std::min<int64_t>(R, rows) * Dh * 4;
+        const float last = units <= LPP_COUNTER_SLOTS ? join_last(bytes) : INFINITY, launch = join_launch(bytes * (double)units);
+        later = launch < last;
+        t += std::min(last, launch);
+      }
+      if (t < best) {
+        best = t;
+        p.shape = i; p.rows = rows; p.kt = h.kt; p.wk = h.wk;
+        p.row_blocks = (int)row_blocks; p.nsplit = (int)ranges; p.range = (int)(per * h.wk); p.join_later = later;
+        const size_t merge = h.wk > 1 ? (size_t)h.wk * rows * (Dh + 4) * sizeof(float) : 0;
+        p.lds = std::max((size_t)h.st * h.wk * 2 * h.kt * Dh * 2, merge);
+      }
+    }
   }
-  p.row_blocks = (int)((R + p.rows - 1) / p.rows);
-  const int64_t units = B * cache->Hkv * p.row_blocks;
-  const int64_t tiles = (S + p.kt - 1) / p.kt + (M + p.kt - 1) / p.kt, rounds = (tiles + p.wk - 1) / p.wk;
-  // key ranges only while compute units would idle, of two rounds of the block's waves at least
-  int64_t ranges = std::min<int64_t>((int64_t)cache->n_cu * resident / std::max<int64_t>(units, 1), rounds / 2);
-  if (units > LPP_COUNTER_SLOTS) ranges = 1;
-  ranges = std::max<int64_t>(1, std::min<int64_t>(ranges, ((int64_t)1 << 31) / (units * p.rows * (Dh + 2) * 4) - 1));
-  const int64_t per = (rounds + ranges - 1) / ranges;
-  p.range = (int)(per * p.wk);
-  p.nsplit = (int)((tiles + p.range - 1) / p.range);
-  const size_t parts = p.nsplit > 1 ? (size_t)units * p.nsplit * p.rows : 0;
+  const size_t parts = p.nsplit > 1 ? (size_t)heads * p.row_blocks * p.nsplit * p.rows : 0;
   p.o_bytes = lpp_align_up(parts * Dh * sizeof(float), 256);
   p.ml_bytes = lpp_align_up(parts * 2 * sizeof(float), 256);
   return p;
@@ -735,21 +868,40 @@ int32_t launch(K kern, LppLdsLimit& limit, const PagedAttnArgs& a, int threads, 
   LPP_HIP_TRY(hipGetLastError());
   return LPP_OK;
 }
-template <int DH, int NT, int WR, int WK, int KT>
+template <int DH, int ROWS, bool BF16>
+int32_t launch_join(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
+  if (!a.join_later) return LPP_OK;
+  const uint32_t tiles = a.units / (uint32_t)a.nsplit * (uint32_t)a.row_blocks;
+  constexpr int C4 = DH / 4;
+  if (a.nsplit <= 8) hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 2, BF16>), dim3(tiles * (ROWS * C4 * 2 / 256)), dim3(256), 0, s, a, p.kt);
+  else hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 256 / C4, BF16>), dim3(tiles * ROWS), dim3(256), 0, s, a, p.kt);
+  LPP_HIP_TRY(hipGetLastError());
+  return LPP_OK;
+}
+template <int DH, int SHAPE>
 int32_t launch_bf16(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   static LppLdsLimit limit;
-  return launch(paged_attn_bf16_kernel<DH, NT, WR, WK, KT>, limit, a, WR * WK * 64, p, s);
+  constexpr Shape h = kShapes[SHAPE];
+  const int32_t st = launch(paged_attn_bf16_kernel<DH, h.wr, h.wk, h.kt, h.st>, limit, a, h.wr * h.wk * 64, p, s);
+  return st != LPP_OK ? st : launch_join<DH, h.wr * 32, true>(a, p, s);
 }
-template <int DH, int W>
+template <int DH, int NT>
 int32_t launch_f32(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   static LppLdsLimit limit;
-  return launch(paged_attn_f32_kernel<DH, W>, limit, a, W * 64, p, s);
+  constexpr int W = DH == 64 && NT == 1 ? 16 : 8;
+  const int32_t st = launch(paged_attn_f32_kernel<DH, NT, W>, limit, a, W * 64, p, s);
+  return st != LPP_OK ? st : launch_join<DH, NT * 16, false>(a, p, s);
 }
 template <int DH>
 int32_t launch_paged(const lpp_paged* cache, const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
-  if (cache->dtype == LPP_F32) return launch_f32<DH, DH == 64 ? 16 : 8>(a, p, s);
-  if (p.wr == 4) return launch_bf16<DH, 1, 4, 1, 64>(a, p, s);
-  return p.nt == 1 ? launch_bf16<DH, 1, 1, 4, 32>(a, p, s) : launch_bf16<DH, 2, 1, 4, 32>(a, p, s);
+  if (cache->dtype == LPP_F32) return p.shape == 0 ? launch_f32<DH, 1>(a, p, s) : launch_f32<DH, 2>(a, p, s);
+  switch (p.shape) {
+    case 0: return launch_bf16<DH, 0>(a, p, s);
+    case 1: return launch_bf16<DH, 1>(a, p, s);
+    case 2: return launch_bf16<DH, 2>(a, p, s);
+    case 3: return launch_bf16<DH, 3>(a, p, s);
+    default: return launch_bf16<DH, 4>(a, p, s);
+  }
 }
 
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
@@ -790,6 +942,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   a.ws_ml = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(ws) + p.o_bytes);
   a.ws_o_bytes = (uint32_t)p.o_bytes; a.ws_ml_bytes = (uint32_t)p.ml_bytes;
   a.counters = cache->d_counters;
+  a.join_later = p.join_later;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return cache->Dh == 64 ? launch_paged<64>(cache, a, p, s) : launch_paged<128>(cache, a, p, s);
 }
