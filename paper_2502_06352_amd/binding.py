@@ -327,21 +327,29 @@ def lpp_relaxed_verify_sampled(tree: Tree, cond_logits, uncond_logits, cfg_scale
 # The calls below take tensors of the shapes that include/lpp.h states and say so if one is of another size or type, lies
 # on another device than the current one, or has gaps: the kernels go by sizes alone.
 _DTYPES = None
+_current = _raw = None    # the current device's number, and the raw handle of a device's current stream, once there is a device
 
 
 def _device() -> int:
-    """The current HIP device, and the element types by their number."""
-    global _torch, _DTYPES
+    """The current HIP device (-1: there is none)."""
+    global _DTYPES, _current, _raw
+    if _current is not None:
+        return _current()
+    import torch
     if _DTYPES is None:
-        import torch
-        _torch = torch
         _DTYPES = {LPP_F32: torch.float32, LPP_BF16: torch.bfloat16, "i32": torch.int32, "f32": torch.float32}
-    c = _torch.cuda
-    return c.current_device() if c.is_initialized() or c.is_available() else -1
+    if not torch.cuda.is_available():
+        return -1
+    device = torch.cuda.current_device()       # (initialises)
+    _raw = getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cuda.current_stream(d).cuda_stream)
+    _current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return device
 
 
 def _on(stream, device: int) -> Optional[int]:
-    return None if device < 0 and stream is None else _stream(stream)
+    if stream is not None:
+        return _stream(stream)
+    return None if device < 0 else _raw(device) or None
 
 
 def _refuse(where: str, what: str):
@@ -350,13 +358,9 @@ def _refuse(where: str, what: str):
 
 def _want(where: str, name: str, t, dtype, n: int, device: int) -> int:
     """Address of ``t``, which is to be ``n`` contiguous elements on ``device``."""
-    if t.get_device() != device:
-        _refuse(where, f"{name} is not on the current device")
-    if t.dtype is not _DTYPES.get(dtype):
-        _refuse(where, f"{name} has the wrong element type")
-    if t.numel() != n or not t.is_contiguous():
-        _refuse(where, f"{name} has another size, or gaps")
-    return t.data_ptr()
+    if t.dtype is _DTYPES.get(dtype) and t.numel() == n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    _refuse(where, f"{name} is of another type or size, has gaps, or is not on the current device")
 
 
 def _maybe(where: str, name: str, t, dtype, n: int, device: int) -> Optional[int]:
@@ -480,14 +484,11 @@ def _rows_in(where: str, name: str, t, dtype, B: int, M: int, heads: int, Dh: in
     """lpp_rows of a [B, M, heads, Dh] tensor of any strides but the last."""
     if t is None:
         return None
-    if tuple(t.shape) != (B, M, heads, Dh):
-        _refuse(where, f"{name} is not [B, M, heads, Dh]")
-    if t.get_device() != device or t.dtype is not _DTYPES.get(dtype):
-        _refuse(where, f"{name} is not on the current device, or of another element type")
-    item, row, head, one = t.stride()
-    if one != 1:
-        _refuse(where, f"the numbers of a head of {name} do not follow each other")
-    return _pack_rows(t.data_ptr(), item, row, head)
+    if t.shape == (B, M, heads, Dh) and t.dtype is _DTYPES.get(dtype) and t.get_device() == device:
+        item, row, head, one = t.stride()
+        if one == 1 or Dh == 1:
+            return _pack_rows(t.data_ptr(), item, row, head)
+    _refuse(where, f"{name} is not [B, M, heads, Dh] of that type on the current device, the numbers of a head one behind the other")
 
 
 def lpp_rotary_qkv(rotary: Rotary, tree: Optional[Tree], dtype: int, q, k, v, first_pos, row_len, B: int, H: int, Hkv: int,

@@ -803,16 +803,17 @@ struct Shape { int wr, wk, kt, st; int resident[2]; float alone[2], each[2]; };
 constexpr Shape kShapes[] = {
     {1, 4, 32, 1, {4, 2}, {0.83f, 1.32f}, {0.37f, 1.10f}},
     {1, 8, 32, 1, {2, 1}, {0.84f, 1.22f}, {0.79f, 1.86f}},
-    {2, 4, 32, 2, {2, 1}, {0.87f, 0.93f}, {0.62f, 1.41f}},
+    {2, 4, 32, 2, {2, 1}, {0.87f, 0.93f}, {0.60f, 1.41f}},
     {4, 1, 64, 2, {3, 2}, {0.97f, 1.94f}, {0.60f, 0.50f}},
     {4, 2, 32, 2, {2, 1}, {0.76f, 1.00f}, {0.62f, 1.10f}},
 };
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
 
 // What adding up the ranges of a launch costs: by the block that finishes last (bytes: of a row tile) or in a launch of its own, which
-// reads with all compute units.  (1 head, 108 rows, 21419 keys in 32 ranges: 34 us and 19; 8 heads, 4 rows, 2400 keys in 6: 12.4 and 12.7.)
-inline float join_last(double bytes) { return 3.2f + (float)(bytes / 18900.); }
-inline float join_launch(double bytes) { return 3.4f + (float)(bytes / 1540000.); }
+// reads with all compute units but costs a caller without a graph another 4 us of host time.  (1 head, 108 rows, 21419 keys in 16 ranges: 32.6 us
+// and 23.1, replayed; 8 heads, 4 rows, 2400 keys in 10: 10.7 and 10.4.)
+inline float join_last(float bytes) { return 3.2f + bytes / 18900.f; }
+inline float join_launch(float bytes) { return 6.f + bytes / 1540000.f; }
 
 // The shape and the number of ranges whose estimate is least: rounds of a block, each as long as a compute unit takes with the
 // blocks that fall to it, a fixed cost for every block there, and the joining.  Over the inputs above the choices take 1.02 times the best of
@@ -823,35 +824,38 @@ PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64
   const int Dh = cache->Dh, d = Dh == 128;
   const bool bf16 = cache->dtype == LPP_BF16;
   const Shape f32[2] = {{1, Dh == 64 ? 16 : 8, 16, 0, {1, 1}, {3.3f, 3.2f}, {3.1f, 3.2f}}, {2, 8, 16, 0, {1, 1}, {3.0f, 5.2f}, {2.9f, 5.5f}}};
-  double best = INFINITY;
+  float best = INFINITY;
   for (int i = 0; i < (bf16 ? (int)(sizeof(kShapes) / sizeof(kShapes[0])) : 2); ++i) {
     const Shape& h = bf16 ? kShapes[i] : f32[i];
     const int rows = h.wr * (bf16 ? 32 : 16);
+    if (i > 0 && h.wr > 1 && R <= rows / 2) break;   // (no block has more rows than the next smaller one would)
     const int64_t row_blocks = (R + rows - 1) / rows, units = heads * row_blocks;
-    const int64_t tiles = (S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt, rounds = (tiles + h.wk - 1) / h.wk;
-    int64_t before = 0;
+    const int tiles = (int)((S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt), rounds = (tiles + h.wk - 1) / h.wk;
+    int before = 0;
     for (const int g : kRanges) {
-      const int64_t per = (rounds + std::min<int64_t>(g, rounds) - 1) / std::min<int64_t>(g, rounds), ranges = (rounds + per - 1) / per, blocks = units * ranges;
+      const int per = (rounds + std::min(g, rounds) - 1) / std::min(g, rounds), ranges = (rounds + per - 1) / per;
       if (ranges == before) continue;                // (as many as the last choice)
       before = ranges;
+      const int64_t blocks = units * ranges;
       if (ranges > 1 && blocks * rows * (Dh + 2) * 4 >= (int64_t)1 << 31) break;      // (32-bit offsets into the parts)
-      const int64_t k = (blocks + cache->n_cu - 1) / cache->n_cu;
-      const double load = std::max(1., (double)blocks / cache->n_cu);
-      double t = (double)per * std::max<double>(h.alone[d] * (double)((k + h.resident[d] - 1) / h.resident[d]), h.each[d] * load) + 0.7 * (double)k;
+      const float each = (float)blocks / (float)cache->n_cu, k = ceilf(each);
+      const float load = 0.75f * std::max(1.f, each) + 0.25f * k;      // (between the average and the fullest)
+      float t = (float)per * std::max(h.alone[d] * ceilf(k / (float)h.resident[d]), h.each[d] * load) + 0.7f * k;
       bool later = false;
       if (ranges > 1) {
-        const double bytes = (double)ranges * (double)std::min<int64_t>(R, rows) * Dh * 4;
-        const float last = units <= LPP_COUNTER_SLOTS ? join_last(bytes) : INFINITY, launch = join_launch(bytes * (double)units);
+        const float bytes = (float)ranges * (float)std::min<int64_t>(R, rows) * (float)(Dh * 4);
+        const float last = units <= LPP_COUNTER_SLOTS ? join_last(bytes) : INFINITY, launch = join_launch(bytes * (float)units);
         later = launch < last;
         t += std::min(last, launch);
       }
       if (t < best) {
         best = t;
         p.shape = i; p.rows = rows; p.kt = h.kt; p.wk = h.wk;
-        p.row_blocks = (int)row_blocks; p.nsplit = (int)ranges; p.range = (int)(per * h.wk); p.join_later = later;
+        p.row_blocks = (int)row_blocks; p.nsplit = ranges; p.range = per * h.wk; p.join_later = later;
         const size_t merge = h.wk > 1 ? (size_t)h.wk * rows * (Dh + 4) * sizeof(float) : 0;
         p.lds = std::max((size_t)h.st * h.wk * 2 * h.kt * Dh * 2, merge);
       }
+      if (per == 1 || (ranges > 1 && each > 8.f)) break;
     }
   }
   const size_t parts = p.nsplit > 1 ? (size_t)heads * p.row_blocks * p.nsplit * p.rows : 0;

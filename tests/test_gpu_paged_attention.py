@@ -194,8 +194,9 @@ def test_pages_beyond_four_gigabytes(dtype):
 
 def test_two_runs_give_the_same_bits_and_leave_the_handle_clean():
     """Key ranges joined by the block that finishes last; other sizes on the same handle and workspace in between."""
-    c = Case(1, 8, 2, 128, 16, [700], parent=TINY, seed=7)
+    c = Case(1, 8, 2, 128, 16, [3000], parent=TINY, seed=7)
     t = c.upload()
+    assert t["ws"].numel() > 256
     first = c.call(t).clone()
     d = Case(1, 8, 2, 128, 16, [90], M=70, rows=[70], seed=8)
     u = d.upload()
@@ -210,8 +211,18 @@ def test_two_runs_give_the_same_bits_and_leave_the_handle_clean():
     c.check(first)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(B=1, H=2, Hkv=1, Dh=128, page=64, lens=[9000], parent=XXL),
+                                dict(B=2, H=4, Hkv=2, Dh=64, page=16, lens=[7000, 300], M=33, rows=[33, 20]),
+                                dict(B=3, H=1, Hkv=1, Dh=64, page=256, lens=[20000, 5, 9999], parent=[-1])])
+def test_many_ranges(kw, dtype):
+    """Long caches of few heads: ranges added up by the last block or in a launch of their own, items of one range beside others."""
+    t = Case(dtype=dtype, seed=10, **kw).run()
+    assert t["ws"].numel() > 256
+
+
 def test_a_short_workspace_is_refused():
-    c = Case(1, 8, 2, 128, 16, [700], parent=TINY)
+    c = Case(1, 8, 2, 128, 16, [3000], parent=TINY)
     t = c.upload()
     assert t["ws"].numel() > 256                                    # (the keys are cut in ranges here)
     for ws in (t["ws"][:-256], None):
