@@ -71,7 +71,7 @@ struct RotaryArgs {
   int32_t words, M, Dh, dim;
   int32_t rows, units, row_blocks;   // rows of a block, lanes of a row, blocks of an item
   int32_t heads_q, heads_qk, heads;  // H, H + Hkv, H + 2 Hkv (what is missing counts none)
-  int32_t group;                     // heads of a block
+  int32_t group, groups;             // heads of a block; blocks of some rows
   int32_t n_heads[3];
   float magnitude;
   double turns[LPP_ROTARY_MAX_DIM / 2];
@@ -103,14 +103,15 @@ template <> struct Eight<float> {
 
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  const int b = (int)(blockIdx.x / (unsigned)a.row_blocks), rb = (int)(blockIdx.x - (unsigned)b * a.row_blocks);
+  const int id = (int)(blockIdx.x / (unsigned)a.groups), group = (int)(blockIdx.x - (unsigned)id * a.groups);
+  const int b = id / a.row_blocks, rb = id - b * a.row_blocks;
   const int r = (int)threadIdx.x / a.units, u = (int)threadIdx.x - r * a.units;
   const int i = rb * a.rows + r;
   const int n = a.row_len ? min(max(a.row_len[b], 0), a.M) : a.M;
   if (r >= a.rows || i >= n) return;
   const bool turned = u * 16 < a.dim;
   const int e0 = HALF && turned ? 8 * u : 16 * u, e1 = HALF && turned ? a.dim / 2 + 8 * u : 16 * u + 8;
-  const int h0 = (int)blockIdx.y * a.group, h1 = min(h0 + a.group, a.heads);
+  const int h0 = group * a.group, h1 = min(h0 + a.group, a.heads);
   float cs[8], sn[8];
   if (turned && h0 < a.heads_qk) {
     int64_t pos = a.first_pos ? a.first_pos[b] : 0;
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
       sn[j] = a.magnitude * s;
     }
   }
-  constexpr int UN = 4;                              // heads in flight
+  constexpr int UN = 2;                              // heads in flight
   for (int h = h0; h < h1; h += UN) {
     Eight<T> x[UN][2];
 #pragma unroll
@@ -221,12 +222,13 @@ extern "C" int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree
   a.M = M; a.Dh = Dh; a.dim = rotary->dim; a.magnitude = rotary->magnitude;
   a.units = Dh / 16; a.rows = std::min(256 / a.units, M);
   a.row_blocks = (M + a.rows - 1) / a.rows;
-  a.group = 8;
+  // (two heads a block, blocks of some rows one behind the other, so that what lies together is read together)
+  a.group = 2;
+  a.groups = (a.heads + a.group - 1) / a.group;
   std::copy(rotary->turns, rotary->turns + LPP_ROTARY_MAX_DIM / 2, a.turns);
-  const int64_t blocks = (int64_t)B * a.row_blocks;
-  const int groups = (a.heads + a.group - 1) / a.group;
-  if (blocks > 0x7FFFFFFF || groups > 65535) return LPP_EUNSUPPORTED;
-  const dim3 grid((unsigned)blocks, (unsigned)groups);
+  const int64_t blocks = (int64_t)B * a.row_blocks * a.groups;
+  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  const dim3 grid((unsigned)blocks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool half = rotary->layout == LPP_ROTARY_HALF;
   if (dtype == LPP_BF16) {
