@@ -44,6 +44,8 @@ struct PagedAttnArgs {
   uint32_t rc_gq;
   int32_t table_stride, page_shift, n_pages;
   int32_t row_blocks, nsplit, range; // blocks of rows of a (item, head); ranges of its keys, of so many tiles
+  int32_t share;                     // items (at most 64) that are looked at by their own lengths: with ranges these are cut by them, without
+                                     // the longest begin; 0: every item has nsplit ranges and its turn
   uint32_t units, whole;             // (item, head, range), and how many of them in eights
   float scale;                       // bf16: times log2 e
   float* ws_o;                       // [item, head, row block][nsplit][ROWS][Dh] unnormalised parts
@@ -53,13 +55,73 @@ struct PagedAttnArgs {
   int32_t join_later;                // ranges are joined by a kernel of their own
 };
 
+// Sum of x over this lane and those before it.
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);     // row_shr:1, 2, 4, 8: inside sixteen lanes
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);     // row_bcast:15 into the second and fourth sixteen
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);     // row_bcast:31 into the upper half
+  return x;
+}
+
+// The items' lengths, lane i has item i's: cached keys, new rows, and the tiles of both.
+struct Lengths {
+  int seq, rows;
+  uint32_t tiles;
+  __device__ __forceinline__ Lengths(const PagedAttnArgs& a, int kt) {
+    const int i = min((int)(threadIdx.x & 63), a.share - 1);
+    seq = a.seq_len ? min(max(a.seq_len[i], 0), a.S) : a.S;
+    rows = a.row_len ? min(max(a.row_len[i], 0), a.M) : a.M;
+    tiles = rows > 0 ? (uint32_t)((seq + kt - 1) / kt + (rows + kt - 1) / kt) : 0u;
+  }
+};
+
+// The item whose turn is number `turn` when the longest begin, so that what is left at the end is short.  (8 chunks of 512 rows, 32 heads
+// over 8 of 128 numbers, up to 8192 keys: in the batch's order 335 us if that is the shortest first, 279 shuffled, 264 the longest first;
+// so 262 in any order.  16 trees of 129 rows, 24 heads over 8 of 64, up to 4096 keys: 71.8, 67.7 and 62.5; so 63.3.)
+__device__ __forceinline__ int longest_first(const Lengths& len, int items, int turn) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int j = 0; j < items; ++j) {
+    const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)len.tiles, j);
+    before += t > len.tiles || (t == len.tiles && j < lane) ? 1 : 0;
+  }
+  return __ffsll(__ballot(before == turn && lane < items)) - 1;
+}
+
+// Ranges cut by the lengths that the device alone knows: the plan's blocks are for items of S keys each, and where items are shorter
+// the same blocks take ranges as much shorter, down to half (an item then has up to twice as many, which one block may have to
+// add up).  All items' ranges are of one size, the least that leaves no more ranges than there are blocks.  Lane i has item i.
+// (16 single tokens, 32 heads over 8 of 128 numbers, 2048 to 32768 keys: 206 us, 227 with ranges for 32768 keys.)
+struct Shares {
+  uint32_t n, end;                   // my item's ranges, and those of all items up to it
+  int range;                         // tiles
+  __device__ __forceinline__ Shares(const PagedAttnArgs& a, const Lengths& len, int wk) {
+    const uint32_t tiles = (int)(threadIdx.x & 63) < a.share ? len.tiles : 0u;
+    const uint32_t rounds = (tiles + (uint32_t)wk - 1) / (uint32_t)wk, slots = (uint32_t)(a.share * a.nsplit);
+    const uint32_t most = (uint32_t)(a.range / wk), all = (uint32_t)__builtin_amdgcn_readlane((int)sum_up_to(rounds), 63);
+    uint32_t per = max((most + 1) / 2, (all + slots - 1) / slots);
+    for (;; per = min(most, per + max(per >> 3, 1u))) {              // (at `most` no item has more than nsplit)
+      n = (rounds + per - 1) / per;
+      end = sum_up_to(n);
+      if (per >= most || (uint32_t)__builtin_amdgcn_readlane((int)end, 63) <= slots) break;
+    }
+    range = (int)per * wk;
+  }
+  __device__ __forceinline__ int item_of(uint32_t u) const { return __popcll(__ballot(end <= u)); }   // whose range is number u
+  __device__ __forceinline__ uint32_t ranges(int b) const { return (uint32_t)__builtin_amdgcn_readlane((int)n, b); }
+  __device__ __forceinline__ uint32_t before(int b) const { return (uint32_t)__builtin_amdgcn_readlane((int)(end - n), b); }
+};
+
 // What a block works on.  The row blocks of a (item, head, range) read the same keys and sit on one XCD (block index mod 8) one
 // behind the other, as long as there are eight such units; the rest spread over the XCDs.
 struct Cell {
-  int b, kvh, kvbh, rb, split;
+  int b, kvh, kvbh, rb, split, range;
   int seq, rows;                     // cached keys, new rows of the item
-  bool live;
-  __device__ __forceinline__ explicit Cell(const PagedAttnArgs& a) {
+  uint32_t part;                     // the row tile's parts in the workspace: the first one's number
+  __device__ __forceinline__ explicit Cell(const PagedAttnArgs& a, int kt, int wk) {
     const uint32_t id = blockIdx.x, RB = (uint32_t)a.row_blocks;
     uint32_t u;
     if (id < a.whole * RB) {
@@ -71,13 +133,38 @@ struct Cell {
       rb = (int)(t / left);
       u = a.whole + t - (uint32_t)rb * left;
     }
-    kvbh = (int)(u / (uint32_t)a.nsplit);
-    split = (int)(u - (uint32_t)kvbh * (uint32_t)a.nsplit);
-    b = kvbh / a.Hkv;
-    kvh = kvbh - b * a.Hkv;
-    seq = a.seq_len ? min(max(a.seq_len[b], 0), a.S) : a.S;
-    rows = a.row_len ? min(max(a.row_len[b], 0), a.M) : a.M;
+    range = a.range;
+    uint32_t n = (uint32_t)a.nsplit, first;          // the item's ranges, the units before it
+    if (a.share && n == 1) {
+      const Lengths len(a, kt);
+      b = longest_first(len, a.share, (int)(u / (uint32_t)a.Hkv));
+      first = u / (uint32_t)a.Hkv * (uint32_t)a.Hkv;
+      seq = __builtin_amdgcn_readlane(len.seq, b);
+      rows = __builtin_amdgcn_readlane(len.rows, b);
+    } else if (a.share) {
+      const Lengths len(a, kt);
+      const Shares sh(a, len, wk);
+      b = sh.item_of(u / (uint32_t)a.Hkv);
+      if (b >= a.share) {                            // behind the last range
+        b = kvh = kvbh = split = seq = rows = 0;
+        return;
+      }
+      range = sh.range;
+      n = sh.ranges(b);
+      first = sh.before(b) * (uint32_t)a.Hkv;
+      seq = __builtin_amdgcn_readlane(len.seq, b);
+      rows = __builtin_amdgcn_readlane(len.rows, b);
+    } else {
+      b = (int)(u / (n * (uint32_t)a.Hkv));
+      first = (uint32_t)b * n * (uint32_t)a.Hkv;
+      seq = a.seq_len ? min(max(a.seq_len[b], 0), a.S) : a.S;
+      rows = a.row_len ? min(max(a.row_len[b], 0), a.M) : a.M;
+    }
+    kvh = (int)((u - first) / n);
+    split = (int)(u - first - (uint32_t)kvh * n);
+    kvbh = b * a.Hkv + kvh;
     if (!a.anc) rb = a.row_blocks - 1 - rb;          // a chunk's last rows see most: first
+    part = (first + (uint32_t)kvh * n) * RB + (uint32_t)rb * n;
   }
 };
 
@@ -143,7 +230,7 @@ __device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& 
   if (s_ticket != ns - 1) return;
   constexpr int C4 = DH / 4;
   const __amdgpu_buffer_rsrc_t dev_o = device_buffer(a.ws_o, a.ws_o_bytes), dev_ml = device_buffer(a.ws_ml, a.ws_ml_bytes);
-  const uint32_t part0 = (uint32_t)tile * (uint32_t)a.nsplit * ROWS;
+  const uint32_t part0 = c.part * ROWS;
   for (int idx = threadIdx.x; idx < ROWS * C4; idx += THREADS) {
     const int r = idx / C4, c4 = idx % C4;
     if (r0 + r >= R) continue;
@@ -185,7 +272,7 @@ __device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& 
 // The same for parts that are many, in a launch of its own: a lane has four numbers of a share of a row's ranges, shares are added in
 // their order.
 template <int DH, int ROWS, int SHARES, bool BF16>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int tiles_of_keys) {
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int kt, int wk) {
   constexpr int C4 = DH / 4, RPB = 256 / (C4 * SHARES), BPT = ROWS / RPB;    // rows of a block, blocks of a row tile
   __shared__ __align__(16) float4 s_o[RPB][SHARES][C4];
   __shared__ float s_m[RPB][SHARES], s_l[RPB][SHARES];
@@ -196,11 +283,19 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, i
   if (r0 + r - mine >= R) return;
   const int seq = a.seq_len ? min(max(a.seq_len[b], 0), a.S) : a.S;
   const int fresh = (int)div_or_rc((uint32_t)(min(r0 + ROWS, R) - 1), (uint32_t)a.gq, a.rc_gq) + 1;
-  const int T = (seq + tiles_of_keys - 1) / tiles_of_keys + (fresh + tiles_of_keys - 1) / tiles_of_keys;
-  const int ns = (T + a.range - 1) / a.range;
+  const int T = (seq + kt - 1) / kt + (fresh + kt - 1) / kt;
+  int range = a.range;
+  uint32_t n = (uint32_t)a.nsplit, first = (uint32_t)b * n * (uint32_t)a.Hkv;        // as in Cell
+  if (a.share) {
+    const Shares sh(a, Lengths(a, kt), wk);
+    range = sh.range;
+    n = sh.ranges(b);
+    first = sh.before(b) * (uint32_t)a.Hkv;
+  }
+  const int ns = (T + range - 1) / range;
   if (ns == 1) return;                               // (the block wrote its rows itself)
   const int c4 = threadIdx.x % C4, share = threadIdx.x / C4 % SHARES;
-  const int64_t part0 = (int64_t)tile * a.nsplit * ROWS + min(r, R - 1 - r0);
+  const int64_t part0 = (int64_t)((first + (uint32_t)(kvbh - b * a.Hkv) * n) * (uint32_t)a.row_blocks + (uint32_t)rb * n) * ROWS + min(r, R - 1 - r0);
   const float4* po = reinterpret_cast<const float4*>(a.ws_o);
   const float2* pm = reinterpret_cast<const float2*>(a.ws_ml);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -296,7 +391,7 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   __shared__ float s_m[WK][ROWS], s_l[WK][ROWS];
   __shared__ int s_odd;
 
-  const Cell c(a);
+  const Cell c(a, KT, WK);
   const int R = c.rows * a.gq, r0 = c.rb * ROWS;
   if (r0 >= R) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -307,9 +402,9 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   const int fresh = m_last + 1;                      // new keys that the block's rows can see: [0, fresh) (a tree's ancestors come first)
   const int seq = c.seq;
   const int TC = (seq + KT - 1) / KT, T = TC + (fresh + KT - 1) / KT;
-  const int ns = (T + a.range - 1) / a.range;
+  const int ns = (T + c.range - 1) / c.range;
   if (c.split >= ns) return;
-  const int tbeg = c.split * a.range, tend = min(tbeg + a.range, T);
+  const int tbeg = c.split * c.range, tend = min(tbeg + c.range, T);
   if (threadIdx.x == 0) s_odd = 0;
 
   // Q as the B operand: column = row, 8 consecutive Dh a lane and step
@@ -529,7 +624,7 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
         if (tile < tend && !full) clean(tile, base + TILE);
         __syncthreads();
       }
-      if (tile < tend) {
+      if (tile < tend && r0 + wr * 32 < R) {         // (a wave behind the last row only loads)
 #pragma unroll
         for (int kt = 0; kt < SUB; ++kt) {
           bf16x8 pb[2], va[2][DT];
@@ -548,7 +643,7 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   const int new0 = max(tbeg - TC, 0) * KT, new1 = min(max(tend - TC, 0) * KT, fresh);    // new keys of this range
   const uint16_t* vnew = reinterpret_cast<const uint16_t*>(a.vn) + (int64_t)c.kvbh * a.M * DH;
   const __amdgpu_buffer_rsrc_t dev_o = device_buffer(a.ws_o, a.ws_o_bytes), dev_ml = device_buffer(a.ws_ml, a.ws_ml_bytes);
-  const uint32_t part = (uint32_t)((c.kvbh * a.row_blocks + c.rb) * a.nsplit + c.split) * ROWS;
+  const uint32_t part = (c.part + (uint32_t)c.split) * ROWS;
   if (WK == 1) {
     __syncthreads();
     const bool fix = s_odd != 0;
@@ -629,15 +724,15 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
   float4* const s_o = reinterpret_cast<float4*>(smem);      // [W][ROWS][P4]
   __shared__ float s_m[W][ROWS], s_l[W][ROWS];
   __shared__ int s_odd;
-  const Cell c(a);
+  const Cell c(a, 16, W);
   const int R = c.rows * a.gq, r0 = c.rb * ROWS;
   if (r0 >= R) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const int fresh = (int)div_or_rc((uint32_t)(min(r0 + ROWS, R) - 1), (uint32_t)a.gq, a.rc_gq) + 1;
   const int seq = c.seq, TC = (seq + 15) / 16, T = TC + (fresh + 15) / 16;
-  const int ns = (T + a.range - 1) / a.range;
+  const int ns = (T + c.range - 1) / c.range;
   if (c.split >= ns) return;
-  const int tbeg = c.split * a.range, tend = min(tbeg + a.range, T);
+  const int tbeg = c.split * c.range, tend = min(tbeg + c.range, T);
   if (threadIdx.x == 0) s_odd = 0;
   int row[NT];
   f32x4 q[NT][DH / 16], acc[NT][4 * HT];
@@ -754,7 +849,7 @@ __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a)
   __syncthreads();
 
   const __amdgpu_buffer_rsrc_t dev_o = device_buffer(a.ws_o, a.ws_o_bytes), dev_ml = device_buffer(a.ws_ml, a.ws_ml_bytes);
-  const uint32_t part = (uint32_t)((c.kvbh * a.row_blocks + c.rb) * a.nsplit + c.split) * ROWS;
+  const uint32_t part = (c.part + (uint32_t)c.split) * ROWS;
   for (int idx = threadIdx.x; idx < ROWS * DH / 4; idx += W * 64) {
     const int r = idx / (DH / 4), c4 = idx % (DH / 4);
     if (r0 + r >= R) continue;
@@ -877,8 +972,8 @@ int32_t launch_join(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   if (!a.join_later) return LPP_OK;
   const uint32_t tiles = a.units / (uint32_t)a.nsplit * (uint32_t)a.row_blocks;
   constexpr int C4 = DH / 4;
-  if (a.nsplit <= 8) hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 2, BF16>), dim3(tiles * (ROWS * C4 * 2 / 256)), dim3(256), 0, s, a, p.kt);
-  else hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 256 / C4, BF16>), dim3(tiles * ROWS), dim3(256), 0, s, a, p.kt);
+  if (a.nsplit <= 8) hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 2, BF16>), dim3(tiles * (ROWS * C4 * 2 / 256)), dim3(256), 0, s, a, p.kt, p.wk);
+  else hipLaunchKernelGGL((paged_attn_join_kernel<DH, ROWS, 256 / C4, BF16>), dim3(tiles * ROWS), dim3(256), 0, s, a, p.kt, p.wk);
   LPP_HIP_TRY(hipGetLastError());
   return LPP_OK;
 }
@@ -940,6 +1035,12 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   a.rc_gq = reciprocal((uint32_t)gq, (uint64_t)M * gq);
   a.table_stride = table_stride; a.page_shift = cache->page_shift; a.n_pages = cache->n_pages;
   a.row_blocks = p.row_blocks; a.nsplit = p.nsplit; a.range = p.range;
+  // Lengths are looked at where blocks are long enough to pay for it (half a microsecond each): ranges of three rounds or more in
+  // launches of up to two blocks a compute unit, which shorter ranges fill better (3 items, 48 heads over 12 of 128, 277 rows, 708 to 2124
+  // keys, 972 blocks: 73 us, 86 with shorter ones); without ranges, eight rounds or more in launches that do not fit at once.
+  const int64_t blocks = units * p.row_blocks, n_cu = cache->n_cu;
+  const int per = p.range / p.wk;
+  a.share = B > 1 && B <= 64 && (seq_len || row_len) && (p.nsplit > 1 ? per >= 3 && blocks <= 2 * n_cu : per >= 8 && blocks > n_cu) ? B : 0;
   a.units = (uint32_t)units; a.whole = (uint32_t)(units & ~7ll);
   a.scale = cache->dtype == LPP_F32 ? scale : scale * 1.44269504088896340736f;
   a.ws_o = reinterpret_cast<float*>(ws);

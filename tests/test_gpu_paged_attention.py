@@ -258,3 +258,50 @@ def test_captured_on_a_side_stream(kw):
         torch.cuda.synchronize()
         assert torch.equal(t["out"], eager)
     c.check(eager)
+
+
+def _lens(B, most, seed):
+    lens = np.random.default_rng(seed).integers(0, most + 1, B)
+    lens[seed % B], lens[(seed + 1) % B] = most, 0
+    return lens.tolist()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [
+    dict(B=64, H=2, Hkv=1, Dh=64, page=16, lens=_lens(64, 3000, 20), parent=[-1]),
+    dict(B=65, H=1, Hkv=1, Dh=64, page=16, lens=_lens(65, 3000, 21), parent=[-1]),
+    dict(B=7, H=8, Hkv=1, Dh=128, page=32, lens=_lens(7, 6000, 22), M=12, rows=[12, 0, 1, 12, 7, -3, 40]),
+    dict(B=5, H=2, Hkv=2, Dh=64, page=64, lens=[0] * 5, S=6000, parent=XXL),
+    dict(B=6, H=2, Hkv=1, Dh=64, page=64, lens=[0, 1, 0, 9000, 0, 0], parent=TINY),
+    dict(B=3, H=3, Hkv=1, Dh=128, page=128, lens=[50, 14000, 700], M=40, rows=[40, 40, 40]),
+])
+def test_ranges_cut_by_the_items_lengths(kw, dtype):
+    """Items in any order of their lengths, empty ones among them, bounds far above all lengths; batches of 64 and more."""
+    t = Case(dtype=dtype, seed=30, **kw).run()
+    assert t["ws"].numel() > 256
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [
+    dict(B=64, H=8, Hkv=8, Dh=64, page=16, lens=_lens(64, 90, 23), parent=[-1]),
+    dict(B=40, H=8, Hkv=8, Dh=64, page=32, lens=_lens(40, 130, 24), parent=TINY),
+    dict(B=12, H=24, Hkv=8, Dh=128, page=16, lens=_lens(12, 100, 25), M=24, rows=[24, 1, 0, 24, 13, 2, -1, 30, 24, 24, 5, 8]),
+    dict(B=70, H=4, Hkv=4, Dh=64, page=16, lens=_lens(70, 60, 26), parent=[-1]),
+])
+def test_more_items_than_fit_at_once(kw, dtype):
+    """More blocks than compute units, of items in any order of their lengths."""
+    Case(dtype=dtype, seed=31, **kw).run()
+
+
+def test_other_lengths_between_two_runs():
+    """The ranges of one call leave nothing behind for the next, whatever its lengths."""
+    c = Case(4, 4, 1, 128, 16, [6000, 100, 3000, 0], parent=TINY, seed=32)
+    t = c.upload()
+    assert t["ws"].numel() > 256
+    first = c.call(t).clone()
+    c.check(first)
+    for lens in ([0, 0, 0, 0], [1, 100, 2000, 0], [6000, 0, 0, 0], [5999, 90, 2999, 0]):
+        t["lens"].copy_(dev(np.asarray(lens, dtype=np.int32)))
+        c.call(t)
+        t["lens"].copy_(dev(c.lens))
+        assert torch.equal(c.call(t), first)
