@@ -388,10 +388,10 @@ int32_t lpp_paged_destroy(lpp_paged* cache);
 
 /* lpp_commit_kv over pages: row 0 and the accepted path's rows of k_tree / v_tree [device] [B, Hkv, M, Dh] go to positions
  * seq_len[b], seq_len[b] + 1, ...; new_len[b] = seq_len[b] + 1 + accept_len[b].  Capacity is table_stride * page_size: rows
- * at or past it are dropped, lengths are clamped to it.  new_len may be NULL and must not be seq_len itself.
+ * at or past it are dropped, lengths are clamped to it.  new_len may be NULL and must not be one of the inputs.
  * lpp_paged_append_kv: rows 0 .. row_len[b] - 1 of k_new / v_new [device] [B, Hkv, M, Dh] instead (a chunk of a prompt);
  * row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M for every item).
- * Errors: LPP_EINVAL (null, sizes < 1, new_len == seq_len, tensors not 16-byte aligned), LPP_EUNSUPPORTED (capacity + M or the
+ * Errors: LPP_EINVAL (null, sizes < 1, new_len an input, tensors not 16-byte aligned), LPP_EUNSUPPORTED (capacity + M or the
  * launch's blocks beyond 2^31), LPP_EHIP.
  */
 int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* tree, const void* k_tree, const void* v_tree,
@@ -410,7 +410,7 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  *                               written, rows of k_new and v_new behind it not used
  * New rows are not read from the pages: commit or append them before or after.
  *   q [B, H, M, Dh], k_tree / k_new and v_tree / v_new [B, Hkv, M, Dh], out [B, H, M, Dh]   [device] contiguous, of the cache's type,
- *             16-byte aligned; Hkv divides H, query head h reads key/value head h / (H / Hkv)
+ *             16-byte aligned; out overlaps none of the others; Hkv divides H, query head h reads key/value head h / (H / Hkv)
  *   S         [host] no item has more cached positions (seq_len is clamped to it); decides how the launch is cut, so that a bound far
  *             above the lengths costs time.  S = 0: nothing is cached, pages and table may be NULL.  table_stride * page_size >= S
  *   seq_len   [device] int32 [B] or NULL (= S);  row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M)
@@ -419,7 +419,7 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  * Softmax and accumulation are float32; bf16 products run on the bf16 matrix cores with the weights rounded to bf16.  What a row
  * does not see plays no part in it, whatever it holds.  Results do not depend on what is in ws or in pages beyond the lengths, and two
  * calls with the same arguments give the same bits.
- * Errors: LPP_EINVAL (null, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
+ * Errors: LPP_EINVAL (null, out an input, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
  * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, 2^31 blocks), LPP_ENOWORKSPACE,
  * LPP_EHIP.
  */

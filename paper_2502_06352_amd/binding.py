@@ -363,6 +363,15 @@ def _want(where: str, name: str, t, dtype, n: int, device: int) -> int:
     _refuse(where, f"{name} is of another type or size, has gaps, or is not on the current device")
 
 
+def _scratch(where: str, ws, device: int) -> Optional[int]:
+    """Address of a workspace of any type on ``device``."""
+    if ws is None:
+        return None
+    if ws.is_contiguous() and ws.get_device() == device:
+        return ws.data_ptr()
+    _refuse(where, "ws has gaps or is not on the current device")
+
+
 def _maybe(where: str, name: str, t, dtype, n: int, device: int) -> Optional[int]:
     return None if t is None else _want(where, name, t, dtype, n, device)
 
@@ -434,7 +443,7 @@ def lpp_paged_tree_attention(cache: PagedCache, tree: Tree, q, k_pages, v_pages,
     _check(lib().lpp_paged_tree_attention(
         cache.handle, tree.handle, _want(w, "q", q, t, n, d), *_pages(w, cache, k_pages, v_pages, page_table, B, S, d),
         _want(w, "k_tree", k_tree, t, nkv, d), _want(w, "v_tree", v_tree, t, nkv, d),
-        _maybe(w, "seq_len", seq_len, "i32", B, d), B, H, S, scale, _want(w, "out", out, t, n, d), _ptr(ws), _bytes(ws),
+        _maybe(w, "seq_len", seq_len, "i32", B, d), B, H, S, scale, _want(w, "out", out, t, n, d), _scratch(w, ws, d), _bytes(ws),
         _on(stream, d)), w)
 
 
@@ -446,7 +455,7 @@ def lpp_paged_chunk_attention(cache: PagedCache, q, k_pages, v_pages, page_table
         cache.handle, _want(w, "q", q, t, n, d), *_pages(w, cache, k_pages, v_pages, page_table, B, S, d),
         _want(w, "k_new", k_new, t, nkv, d), _want(w, "v_new", v_new, t, nkv, d),
         _maybe(w, "seq_len", seq_len, "i32", B, d), _maybe(w, "row_len", row_len, "i32", B, d), B, H, M, S, scale,
-        _want(w, "out", out, t, n, d), _ptr(ws), _bytes(ws), _on(stream, d)), w)
+        _want(w, "out", out, t, n, d), _scratch(w, ws, d), _bytes(ws), _on(stream, d)), w)
 
 
 LPP_ROTARY_HALF, LPP_ROTARY_INTERLEAVED = 0, 1

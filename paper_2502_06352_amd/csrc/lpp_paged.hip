@@ -39,6 +39,7 @@ extern "C" int32_t lpp_paged_create(int32_t dtype, int32_t Hkv, int32_t Dh, int3
   if (v > 0) c->n_cu = v;
   if (hipMalloc((void**)&c->d_counters, sizeof(int32_t) * LPP_COUNTER_SLOTS) != hipSuccess) return fail();
   if (hipMemset(c->d_counters, 0, sizeof(int32_t) * LPP_COUNTER_SLOTS) != hipSuccess) return fail();
+  if (hipStreamSynchronize(nullptr) != hipSuccess) return fail();            // (whatever stream uses them first)
   *out = c;
   return LPP_OK;
 }
@@ -146,6 +147,7 @@ extern "C" int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* t
                                        int32_t table_stride, const int32_t* seq_len, int32_t B, void* k_pages, void* v_pages,
                                        int32_t* new_len, void* stream) {
   if (!tree || !path || !accept_len) return LPP_EINVAL;
+  if (new_len == accept_len || (new_len && (new_len == path || new_len == page_table))) return LPP_EINVAL;
   PagedWriteArgs a;
   const int32_t st = paged_write(cache, k_tree, v_tree, page_table, table_stride, seq_len, B, tree->M, k_pages, v_pages, new_len, &a);
   if (st != LPP_OK) return st;
@@ -164,6 +166,7 @@ extern "C" int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* t
 extern "C" int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const void* v_new, const int32_t* row_len,
                                        const int32_t* page_table, int32_t table_stride, const int32_t* seq_len, int32_t B,
                                        int32_t M, void* k_pages, void* v_pages, int32_t* new_len, void* stream) {
+  if (new_len && (new_len == row_len || new_len == page_table)) return LPP_EINVAL;
   PagedWriteArgs a;
   const int32_t st = paged_write(cache, k_new, v_new, page_table, table_stride, seq_len, B, M, k_pages, v_pages, new_len, &a);
   if (st != LPP_OK) return st;

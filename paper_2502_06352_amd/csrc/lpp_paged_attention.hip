@@ -1010,6 +1010,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
                         const int32_t* seq_len, const int32_t* row_len, int32_t B, int32_t H, int32_t M, int32_t S, float scale,
                         void* out, void* ws, size_t ws_bytes, void* stream) {
   if (!cache || !q || !k_new || !v_new || !out) return LPP_EINVAL;
+  if (out == q || out == k_new || out == v_new) return LPP_EINVAL;       // blocks read what others have finished
   if (B < 1 || H < 1 || M < 1 || S < 0) return LPP_EINVAL;
   if (S > 0 && (!k_pages || !v_pages || !page_table || table_stride < 1)) return LPP_EINVAL;
   if (H % cache->Hkv != 0) return LPP_EINVAL;

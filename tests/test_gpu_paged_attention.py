@@ -305,3 +305,15 @@ def test_other_lengths_between_two_runs():
         c.call(t)
         t["lens"].copy_(dev(c.lens))
         assert torch.equal(c.call(t), first)
+
+
+def test_tensors_of_the_host_are_refused():
+    """Nothing is enqueued with an address that the kernels cannot read."""
+    c = Case(2, 4, 2, 64, 16, [40, 3], parent=TINY, seed=33)
+    for name in ("ws", "q", "kn", "table", "lens", "out", "kp"):
+        t = c.upload()
+        t[name] = t[name].cpu()
+        with pytest.raises(lpp.LppError) as e:
+            c.call(t)
+        assert e.value.status == lpp.LPP_EINVAL
+    c.run()

@@ -66,6 +66,10 @@ def test_paged_writes_refuse(L):
     def append(c=cache.handle, k=FAKE, v=FAKE, rows=None, table=FAKE, stride=3, seq=FAKE, B=2, M=5, kp=FAKE, vp=FAKE, new=None):
         return L.lpp_paged_append_kv(c, k, v, rows, table, stride, seq, B, M, kp, vp, new, None)
 
+    for other in ("acc", "path", "table", "seq"):
+        _refusals(commit, {}, [({other: 2 * FAKE}, EHIP), ({other: 2 * FAKE, "new": 2 * FAKE}, EINVAL)])
+    for other in ("rows", "table", "seq"):
+        _refusals(append, {}, [({other: 2 * FAKE}, EHIP), ({other: 2 * FAKE, "new": 2 * FAKE}, EINVAL)])
     _refusals(append, {}, shared + [(dict(M=0), EINVAL), (dict(M=0x7FFFFFFF), EUNSUP), (dict(rows=FAKE), EHIP)])
 
 
@@ -74,14 +78,14 @@ def test_paged_attention_refuses(L):
     cache, tree = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0])
 
     def trees(c=cache.handle, t=tree.handle, q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, stride=3, kn=FAKE, vn=FAKE, seq=None, B=2, H=4, S=40,
-              scale=0.0, out=FAKE, ws=FAKE, n=1 << 30):
+              scale=0.0, out=2 * FAKE, ws=FAKE, n=1 << 30):
         return L.lpp_paged_tree_attention(c, t, q, kp, vp, table, stride, kn, vn, seq, B, H, S, scale, out, ws, n, None)
 
     shared = [({}, EHIP), (dict(seq=FAKE), EHIP), (dict(c=None), EINVAL), (dict(q=None), EINVAL), (dict(kp=None), EINVAL), (dict(vp=None), EINVAL),
               (dict(table=None), EINVAL), (dict(stride=0), EINVAL), (dict(stride=2), EINVAL), (dict(kn=None), EINVAL), (dict(vn=None), EINVAL),
               (dict(B=0), EINVAL), (dict(H=0), EINVAL), (dict(H=3), EINVAL), (dict(S=-1), EINVAL), (dict(S=49), EINVAL),
               (dict(S=0, kp=None, vp=None, table=None, stride=0), EHIP), (dict(scale=-1.0), EINVAL), (dict(scale=math.nan), EINVAL),
-              (dict(scale=math.inf), EINVAL), (dict(out=None), EINVAL), (dict(q=FAKE + 4), EINVAL), (dict(out=FAKE + 8), EINVAL),
+              (dict(scale=math.inf), EINVAL), (dict(out=None), EINVAL), (dict(out=FAKE), EINVAL), (dict(q=FAKE + 4), EINVAL), (dict(out=FAKE + 8), EINVAL),
               (dict(kp=FAKE + 2), EINVAL), (dict(B=1 << 24), EUNSUP), (dict(S=1 << 30, stride=1 << 26), EUNSUP)]
     _refusals(trees, {}, shared + [(dict(t=None), EINVAL)])
     need = L.lpp_paged_attention_workspace(cache.handle, 1, 4, 3, 4000)
@@ -91,7 +95,7 @@ def test_paged_attention_refuses(L):
     assert trees(B=1, S=4000, stride=250, n=need) == EHIP
 
     def chunks(c=cache.handle, q=FAKE, kp=FAKE, vp=FAKE, table=FAKE, stride=3, kn=FAKE, vn=FAKE, seq=None, rows=None, B=2, H=4, M=9, S=40,
-               scale=0.0, out=FAKE, ws=FAKE, n=1 << 30):
+               scale=0.0, out=2 * FAKE, ws=FAKE, n=1 << 30):
         return L.lpp_paged_chunk_attention(c, q, kp, vp, table, stride, kn, vn, seq, rows, B, H, M, S, scale, out, ws, n, None)
 
     _refusals(chunks, {}, shared + [(dict(rows=FAKE), EHIP), (dict(M=0), EINVAL), (dict(M=1 << 24), EUNSUP)])
@@ -201,6 +205,13 @@ def test_the_binding_refuses_tensors_of_other_sizes_types_and_strides():
     for bad in (dict(k=new[:1]), dict(k=new.bfloat16()), dict(k=new.transpose(2, 3).contiguous().transpose(2, 3)), dict(kp=pool[:3]),
                 dict(t=table[0]), dict(t=table.long()), dict(s=lens[:1]), dict(p=path[:, :0]), dict(a=lens.float())):
         assert commit(**bad) == EINVAL, bad
+
+    def attend(q=torch.zeros(B, 4, M, Dh), ws=torch.zeros(1 << 16, dtype=torch.uint8), s=lens):
+        return _status(lpp.lpp_paged_tree_attention, cache, tree, q, pool, pool, table, new, new, s, B, 4, 20, 0.0, torch.zeros(B, 4, M, Dh), ws)
+
+    assert attend() == EHIP
+    for bad in (dict(q=new), dict(ws=torch.zeros(1 << 17, dtype=torch.uint8)[::2]), dict(s=lens[:1])):
+        assert attend(**bad) == EINVAL, bad
 
     qkv = torch.zeros(B, M, 8, Dh)
     rotary = lpp.Rotary(32)
