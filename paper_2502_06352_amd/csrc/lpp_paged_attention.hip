@@ -122,6 +122,9 @@ struct Shares {
   __device__ __forceinline__ uint32_t before(int b) const { return (uint32_t)__builtin_amdgcn_readlane((int)(end - n), b); }
 };
 
+// By how much the order of n things turns from one i to the next, i n + j being on XCD number (i n + j) mod 8, so that every j is on all XCDs.
+__device__ __forceinline__ uint32_t turn(uint32_t i, uint32_t n) { return i * min(n & (0u - n), 8u) >> 3; }
+
 // What a block works on.  The row blocks of a (item, head, range) read the same keys and sit on one XCD (block index mod 8) one
 // behind the other, as long as there are eight such units; the rest spread over the XCDs.
 struct Cell {
@@ -168,8 +171,9 @@ struct Cell {
       rows = a.row_len ? min(max(a.row_len[b], 0), a.M) : a.M;
     }
     kvh = (int)((u - first) / n);
-    split = (int)(u - first - (uint32_t)kvh * n);
     kvbh = b * a.Hkv + kvh;
+    // (a head's ranges in an order that turns with the head, so that no XCD has all the first or all the last, which are shorter)
+    split = (int)((u - first - (uint32_t)kvh * n + turn((uint32_t)kvbh, n)) % n);
     if (!a.anc) rb = a.row_blocks - 1 - rb;          // a chunk's last rows see most: first
     part = (first + (uint32_t)kvh * n) * RB + (uint32_t)rb * n;
   }
