@@ -903,15 +903,15 @@ struct PagedPlan {
 };
 
 // Shapes of a bf16 block, and what a round of its waves (kt * wk keys) costs in microseconds: with heads of 64 and of 128 numbers, the
-// block by itself on a compute unit and each of many there.  Measured: 28 shapes of input (1 to 384 heads in all, 4 to 8192 rows, 100
-// to 32768 keys) with 1 to 128 ranges of keys, 1 to 16 ranges joined in both ways; the constants are fitted to those times.
+// block by itself on a compute unit and each of many there.  Fitted to the times of 240 inputs (1 to 384 heads in all, 1 to 8192 rows, 16
+// to 32768 keys, two thirds of the batches of mixed lengths) with 1 to 128 ranges of keys, joined in both ways.
 struct Shape { int wr, wk, kt, st; int resident[2]; float alone[2], each[2]; };
 constexpr Shape kShapes[] = {
-    {1, 4, 32, 1, {4, 2}, {0.83f, 1.32f}, {0.37f, 1.10f}},
-    {1, 8, 32, 1, {2, 1}, {0.84f, 1.22f}, {0.79f, 1.86f}},
-    {2, 4, 32, 2, {2, 1}, {0.87f, 0.93f}, {0.60f, 1.41f}},
-    {4, 1, 64, 2, {3, 2}, {0.97f, 1.94f}, {0.60f, 0.50f}},
-    {4, 2, 32, 2, {2, 1}, {0.76f, 1.00f}, {0.62f, 1.10f}},
+    {1, 4, 32, 1, {4, 2}, {0.87f, 1.16f}, {0.33f, 1.39f}},
+    {1, 8, 32, 1, {2, 1}, {1.23f, 1.19f}, {0.74f, 2.07f}},
+    {2, 4, 32, 2, {2, 1}, {0.87f, 0.89f}, {0.52f, 1.40f}},
+    {4, 1, 64, 2, {3, 2}, {0.95f, 1.25f}, {0.55f, 0.99f}},
+    {4, 2, 32, 2, {2, 1}, {0.74f, 0.76f}, {0.58f, 1.14f}},
 };
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
 
@@ -919,12 +919,13 @@ constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
 // reads with all compute units but costs a caller without a graph another 4 us of host time.  (1 head, 108 rows, 21419 keys in 16 ranges: 32.6 us
 // and 23.1, replayed; 8 heads, 4 rows, 2400 keys in 10: 10.7 and 10.4.)
 inline float join_last(float bytes) { return 3.2f + bytes / 18900.f; }
-inline float join_launch(float bytes) { return 6.f + bytes / 1540000.f; }
+inline float join_launch(float bytes) { return 6.f + bytes / 3090000.f; }
 
 // The shape and the number of ranges whose estimate is least: rounds of a block, each as long as a compute unit takes with the
-// blocks that fall to it, a fixed cost for every block there, and the joining.  Over the inputs above the choices took 1.02 times the best
-// of all measured ones when the constants were fitted (at worst 1.3 times: 12 heads of 879 rows over 2386 keys); blocks of 32, 64 or 128 rows by the
-// number of rows alone took up to 8 times that.
+// blocks that fall to it, or what the memory takes for the keys and values, a fixed cost for every block of a compute unit, and the joining.  Blocks of
+// a chunk longer than any tree see half of the new keys on average, and as they are of all lengths, the longest first, they fill the chip
+// more evenly.  The choices take 1.02 times the best measured one over the inputs above, one in thirty of
+// them more than 1.15 times, at worst 1.29; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8 times that.
 PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64_t S) {
   PagedPlan p{};
   const int64_t R = M * gq, heads = B * cache->Hkv;
@@ -932,12 +933,15 @@ PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64
   const bool bf16 = cache->dtype == LPP_BF16;
   const Shape f32[2] = {{1, Dh == 64 ? 16 : 8, 16, 0, {1, 1}, {3.3f, 3.2f}, {3.1f, 3.2f}}, {2, 8, 16, 0, {1, 1}, {3.0f, 5.2f}, {2.9f, 5.5f}}};
   float best = INFINITY;
+  const float memory = (float)heads * (float)(S + M) * (float)(Dh * (bf16 ? 4 : 8)) / 9.e6f;   // (two thirds of the inputs were shorter than S)
   for (int i = 0; i < (bf16 ? (int)(sizeof(kShapes) / sizeof(kShapes[0])) : 2); ++i) {
     const Shape& h = bf16 ? kShapes[i] : f32[i];
     const int rows = h.wr * (bf16 ? 32 : 16);
     if (i > 0 && h.wr > 1 && R <= rows / 2) break;   // (no block has more rows than the next smaller one would)
     const int64_t row_blocks = (R + rows - 1) / rows, units = heads * row_blocks;
     const int tiles = (int)((S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt), rounds = (tiles + h.wk - 1) / h.wk;
+    const bool causal = M > LPP_MAX_ROWS;
+    const float seen = causal ? 1.f - 0.5f * (float)((M + h.kt - 1) / h.kt) / (float)tiles : 1.f, full = causal ? 0.35f : 0.75f;
     int before = 0;
     for (const int g : kRanges) {
       const int per = (rounds + std::min(g, rounds) - 1) / std::min(g, rounds), ranges = (rounds + per - 1) / per;
@@ -946,8 +950,9 @@ PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64
       const int64_t blocks = units * ranges;
       if (ranges > 1 && blocks * rows * (Dh + 2) * 4 >= (int64_t)1 << 31) break;      // (32-bit offsets into the parts)
       const float each = (float)blocks / (float)cache->n_cu, k = ceilf(each);
-      const float load = 0.75f * std::max(1.f, each) + 0.25f * k;      // (between the average and the fullest)
-      float t = (float)per * std::max(h.alone[d] * ceilf(k / (float)h.resident[d]), h.each[d] * load) + 0.7f * k;
+      const float load = (1.f - full) * std::max(1.f, each * seen) + full * k * seen;      // (between the average and the fullest)
+      const float turns = 1.f + (ceilf(k / (float)h.resident[d]) - 1.f) * seen;
+      float t = std::max((float)per * std::max(h.alone[d] * turns, h.each[d] * load), memory) + 0.87f * k;
       bool later = false;
       if (ranges > 1) {
         const float bytes = (float)ranges * (float)std::min<int64_t>(R, rows) * (float)(Dh * 4);
