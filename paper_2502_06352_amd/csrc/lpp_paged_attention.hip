@@ -574,16 +574,17 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   auto is_full = [&](int tile) { return tile != part_tile && tile < masked0; };
 
   __syncthreads();                                   // (s_odd is cleared before any wave sets it)
+  // Q has arrived before the first load to LDS is issued: a wait for it inside the loop would wait for those as well
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) entry[g] = ahead[g] = 0;
+  look_up(entry, tbeg + kw);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qb[ks]));
   if (tbeg + kw < tend) {                            // (the keys' loads first: they are waited for by their number)
     load_tile(tbeg + kw, 0, true, false);
     load_tile(tbeg + kw, 0, false, true);
   }
   look_up(entry, tbeg + kw + WK);
-  // Q has arrived before the loop: a wait for it in there would wait for the tiles that are on their way as well.  (Here and not before
-  // the first tile is asked for: 8 tokens over 1000 keys, 32 heads over 8 of 128, 11.3 us instead of 12.6; 4 trees of 61 rows over 1024 keys
-  // 11.1 instead of 10.8.)
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qb[ks]));
   if (WR == 1) {
     // A wave by itself, one place for its tile: the next tile's keys go where this one's were as soon as the scores are formed, the values
     // likewise.  (Two places would halve the waves that a compute unit holds; one wave waits where another works.)
