@@ -50,8 +50,9 @@ __device__ __forceinline__ void load4(float (&x)[4], const uint16_t* p) {
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
-// CELLS: groups of four tokens a lane.  Two, or one where blocks of two would be fewer than four a compute unit: 61 guided rows of 8192 4.2 ->
-// 3.5 us; 2064 rows of 16384 62.9 us with two, 68.3 with one, 67.4 with four (4.4 TB/s of the 4.95 that a copy reaches).
+// CELLS: groups of four tokens a lane.  Two, or one where blocks of two would be fewer than four a compute unit: 61 guided rows
+// of 8192 4.2 -> 3.5 us; 2064 rows of 16384 62.9 us with two, 68.3 with one, 67.4 with four (4.4 TB/s of the 4.95 that a copy
+// reaches).
 template <typename T, bool GUIDED, int CELLS>
 __global__ __launch_bounds__(256) void adjust_logits_kernel(LogitsArgs a) {
   constexpr int kCells = CELLS, kPiece = 256 * 4 * CELLS;

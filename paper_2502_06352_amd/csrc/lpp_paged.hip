@@ -1,10 +1,10 @@
 // The paged key/value cache: its handle, and the two calls that write into it.
 //
-// A page holds page_size positions of every key/value head, [Hkv, page_size, Dh]; position p of item b is slot p % page_size
-// of page table[b][p / page_size].  Both calls are pure data movement, 16 bytes a lane, bound by the loads that wait for
-// each other (lengths and path, then the page's number, then the stores; the rows are asked for beside the page's number) where the
-// rows are few (16 items' paths, 24 heads of 64: 2.4 us), and by memory where they are many.  A position whose table entry names no page of the pool is not written: what a read may
-// clamp, a write may not.
+// A page holds page_size positions of every key/value head, [Hkv, page_size, Dh]; position p of item b is slot p % page_size of
+// page table[b][p / page_size].  Both calls are pure data movement, 16 bytes a lane, bound by the loads that wait for each
+// other (lengths and path, then the page's number, then the stores; the rows are asked for beside the page's number) where the
+// rows are few (16 items' paths, 24 heads of 64: 2.4 us), and by memory where they are many.  A position whose table entry
+// names no page of the pool is not written: what a read may clamp, a write may not.
 #include <new>
 
 #include "lpp_internal.h"
@@ -99,8 +99,8 @@ __global__ __launch_bounds__(256) void paged_commit_kernel(PagedWriteArgs a) {
   }
 }
 
-// A block is 256 chunks (16 rows of 256 bytes) of one (item, head), one of K and of V a lane.  (Four of each a lane, 640 blocks in all: 22.6 us
-// for 4 chunks of up to 2048 rows, 8 heads of 128; so 8.7, which is 4.8 TB/s: as fast as a copy.)
+// A block is 256 chunks (16 rows of 256 bytes) of one (item, head), one of K and of V a lane.  (Four of each a lane, 640 blocks
+// in all: 22.6 us for 4 chunks of up to 2048 rows, 8 heads of 128; so 8.7, which is 4.8 TB/s: as fast as a copy.)
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedWriteArgs a) {
   const int bh = (int)(blockIdx.x / (unsigned)a.tiles), tile = (int)(blockIdx.x - (unsigned)bh * a.tiles);
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;

@@ -20,12 +20,13 @@
 // A (item, key/value head)'s keys are cut into ranges where the launch would leave compute units idle; the block of a row tile
 // that finishes last, or a launch of its own, adds the ranges' parts up in their order.
 //
-// What bounds it (replayed; a copy moves 4.95 TB/s here, a large bf16 product reaches 1138 TFLOP/s): single tokens over long caches the memory, 206 us
-// and 5.5 TB/s for 16 items of 2048 to 32768 keys, 32 heads over 8 of 128.  Long chunks the matrix cores' feed, 395 us and 980 TFLOP/s for 2 x 2048
-// rows over 8192 and 4096 keys (matrix cores busy 47 % of the cycles, vector instructions 42 %, no bank conflicts).  Wide trees of heads of 64 the softmax, 62 us and
-// 445 TFLOP/s for 16 trees of 129 rows, 24 heads over 8, up to 4096 keys (vector instructions 55 %, matrix cores 25 %; a tile's 16 exponentials a lane,
-// their products, maxima and sums take longer than its 8 matrix instructions), and there what a compute unit takes in, 53 bytes a ns of
-// the 58 seen at most.  Small calls the latency of one round: 10 us for a token over 2400 keys.
+// What bounds it (replayed; a copy moves 4.95 TB/s here, a large bf16 product reaches 1138 TFLOP/s): single tokens over long
+// caches the memory, 206 us and 5.5 TB/s for 16 items of 2048 to 32768 keys, 32 heads over 8 of 128.  Long chunks the matrix
+// cores' feed, 395 us and 980 TFLOP/s for 2 x 2048 rows over 8192 and 4096 keys (matrix cores busy 47 % of the cycles, vector
+// instructions 42 %, no bank conflicts).  Wide trees of heads of 64 the softmax, 62 us and 445 TFLOP/s for 16 trees of 129
+// rows, 24 heads over 8, up to 4096 keys (vector instructions 55 %, matrix cores 25 %; a tile's 16 exponentials a lane, their
+// products, maxima and sums take longer than its 8 matrix instructions), and there what a compute unit takes in, 53 bytes a ns
+// of the 58 seen at most.  Small calls the latency of one round: 10 us for a token over 2400 keys.
 #include <math.h>
 
 #include <algorithm>
@@ -85,9 +86,10 @@ struct Lengths {
   }
 };
 
-// The item whose turn is number `turn` when the longest begin, so that what is left at the end is short.  (8 chunks of 512 rows, 32 heads
-// over 8 of 128 numbers, up to 8192 keys: in the batch's order 335 us if that is the shortest first, 279 shuffled, 264 the longest first;
-// so 262 in any order.  16 trees of 129 rows, 24 heads over 8 of 64, up to 4096 keys: 71.8, 67.7 and 62.5; so 63.3.)
+// The item whose turn is number `turn` when the longest begin, so that what is left at the end is short.  (8 chunks of 512
+// rows, 32 heads over 8 of 128 numbers, up to 8192 keys: in the batch's order 335 us if that is the shortest first, 279
+// shuffled, 264 the longest first; so 262 in any order.  16 trees of 129 rows, 24 heads over 8 of 64, up to 4096 keys: 71.8,
+// 67.7 and 62.5; so 63.3.)
 __device__ __forceinline__ int longest_first(const Lengths& len, int items, int turn) {
   const int lane = threadIdx.x & 63;
   int before = 0;
@@ -122,7 +124,8 @@ struct Shares {
   __device__ __forceinline__ uint32_t before(int b) const { return (uint32_t)__builtin_amdgcn_readlane((int)(end - n), b); }
 };
 
-// By how much the order of n things turns from one i to the next, i n + j being on XCD number (i n + j) mod 8, so that every j is on all XCDs.
+// By how much the order of n things turns from one i to the next, i n + j being on XCD number (i n + j) mod 8, so that every j
+// is on all XCDs.
 __device__ __forceinline__ uint32_t turn(uint32_t i, uint32_t n) { return i * min(n & (0u - n), 8u) >> 3; }
 
 // What a block works on.  The row blocks of a (item, head, range) read the same keys and sit on one XCD (block index mod 8) one
@@ -226,8 +229,9 @@ __device__ __forceinline__ int64_t row_at(const PagedAttnArgs& a, int kvbh, int 
 template <bool BF16>
 __device__ __forceinline__ float part_weight(float t) { return BF16 ? __builtin_amdgcn_exp2f(t) : exp_neg(t); }
 
-// The parts of a row tile's key ranges, added up in their order by the block that finishes last: every wave waits until its own stores have completed, the barrier gathers the waves, then
-// the ticket is taken; stores, ticket and loads are device-scope, so no cache is written back.
+// The parts of a row tile's key ranges, added up in their order by the block that finishes last: every wave waits until its own
+// stores have completed, the barrier gathers the waves, then the ticket is taken; stores, ticket and loads are device-scope, so
+// no cache is written back.
 template <int DH, int ROWS, int THREADS, bool BF16>
 __device__ __forceinline__ void join_ranges(const PagedAttnArgs& a, const Cell& c, int r0, int R, int ns) {
   __shared__ int s_ticket;
@@ -374,9 +378,9 @@ __device__ __forceinline__ u32x4 buffer_at(uint64_t base) {
   return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0x7FFFFFFFu, 0x00020000u};
 }
 
-// Which 16-byte piece of row `row` piece c of it lies at: c ^ swizzle.  Rows of 128 bytes (8 pieces) and of 256 (16): eight rows
-// that follow each other are at eight places for the first product's reads, and the 64 bytes that the second one reads of each of eight rows fill
-// the banks evenly.
+// Which 16-byte piece of row `row` piece c of it lies at: c ^ swizzle.  Rows of 128 bytes (8 pieces) and of 256 (16): eight
+// rows that follow each other are at eight places for the first product's reads, and the 64 bytes that the second one reads of
+// each of eight rows fill the banks evenly.
 template <int DH>
 __device__ __forceinline__ constexpr int swizzle(int row) {
   return DH == 64 ? ((row >> 1 & 1) << 2) | ((row >> 2 & 1) << 1) | (row >> 3 & 1) : ((row & 3) << 2) | (row >> 2 & 3);
@@ -489,8 +493,9 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
     for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qb[ks], s, 0, 0, 0);
     return s;
   };
-  // Weights of 32 keys: I hold keys 8 (r / 4) + 4 half + r % 4 of column l32.  (One copy of this code for whole tiles and others: with
-  // two, the accumulators were moved from one's registers to the other's, 396 us instead of 378 for two chunks of 2048 rows.)
+  // Weights of 32 keys: I hold keys 8 (r / 4) + 4 half + r % 4 of column l32.  (One copy of this code for whole tiles and
+  // others: with two, the accumulators were moved from one's registers to the other's, 396 us instead of 378 for two chunks of
+  // 2048 rows.)
   auto weights = [&](int tile, int kt, bool full, f32x16 s, bf16x8 (&pb)[2]) {
     if (!full) {
       const bool is_new = tile >= TC;
@@ -569,7 +574,8 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
       }
     }
   };
-  // (only the last tile of the cache, where it is not whole, and new ones: all of a tree's, of a chunk's those that some row of the block is ahead of)
+  // (only the last tile of the cache, where it is not whole, and new ones: all of a tree's, of a chunk's those that some row of
+  // the block is ahead of)
   const int part_tile = seq % KT != 0 ? TC - 1 : T, masked0 = TC + (a.anc ? 0 : (m_first + 1) / KT);
   auto is_full = [&](int tile) { return tile != part_tile && tile < masked0; };
 
@@ -586,8 +592,8 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
   }
   look_up(entry, tbeg + kw + WK);
   if (WR == 1) {
-    // A wave by itself, one place for its tile: the next tile's keys go where this one's were as soon as the scores are formed, the values
-    // likewise.  (Two places would halve the waves that a compute unit holds; one wave waits where another works.)
+    // A wave by itself, one place for its tile: the next tile's keys go where this one's were as soon as the scores are formed,
+    // the values likewise.  (Two places would halve the waves that a compute unit holds; one wave waits where another works.)
     unsigned char* base = smem + kw * 2 * TILE;
     for (int tile = tbeg + kw; tile < tend; tile += WK) {
       const bool more = tile + WK < tend, full = is_full(tile);
@@ -725,9 +731,11 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
 
 // ---------------------------------------------------------------- float32
 
-// A block is NT tiles of 16 rows; its W waves take the 16-key tiles of its range in turn.  Lane (i, g) of a wave holds of key i the
-// dimensions 16 t + 4 g .. + 3, and of keys 4 g + r the values of dimensions 64 h + 4 i .. + 3: what its 16-byte loads bring is what both products
-// want.  Bound by what a compute unit takes in (every block reads all keys of its range): two tiles of rows share what is loaded.
+// A block is NT tiles of 16 rows; its W waves take the 16-key tiles of its range in turn.  Lane (i, g) of a wave holds of key i
+// the dimensions 16 t + 4 g .. + 3, and of keys 4 g + r the values of dimensions 64 h + 4 i .. + 3: what its 16-byte loads
+// bring is what both products want.  Bound by what a compute unit takes in (every block reads all keys of its range: 41 bytes
+// a ns), or, where two tiles of rows share what is loaded, by the float32 matrix instructions (64 % of their rate, by count; 32
+// heads over 8 of 128, 1526 rows over 1380 keys: 602 us, 89 TFLOP/s of the 154 that a large product reaches).
 template <int DH, int NT, int W>
 __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int ROWS = 16 * NT, HT = DH / 64, P4 = DH / 4 + 1;
@@ -902,9 +910,10 @@ struct PagedPlan {
   size_t o_bytes, ml_bytes;          // partials
 };
 
-// Shapes of a bf16 block, and what a round of its waves (kt * wk keys) costs in microseconds: with heads of 64 and of 128 numbers, the
-// block by itself on a compute unit and each of many there.  Fitted to the times of 240 inputs (1 to 384 heads in all, 1 to 8192 rows, 16
-// to 32768 keys, two thirds of the batches of mixed lengths) with 1 to 128 ranges of keys, joined in both ways.
+// Shapes of a bf16 block, and what a round of its waves (kt * wk keys) costs in microseconds: with heads of 64 and of 128
+// numbers, the block by itself on a compute unit and each of many there.  Fitted to the times of 240 inputs (1 to 384 heads in
+// all, 1 to 8192 rows, 16 to 32768 keys, two thirds of the batches of mixed lengths) with 1 to 128 ranges of keys, joined in
+// both ways.
 struct Shape { int wr, wk, kt, st; int resident[2]; float alone[2], each[2]; };
 constexpr Shape kShapes[] = {
     {1, 4, 32, 1, {4, 2}, {0.87f, 1.16f}, {0.33f, 1.39f}},
@@ -915,17 +924,18 @@ constexpr Shape kShapes[] = {
 };
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
 
-// What adding up the ranges of a launch costs: by the block that finishes last (bytes: of a row tile) or in a launch of its own, which
-// reads with all compute units but costs a caller without a graph another 4 us of host time.  (1 head, 108 rows, 21419 keys in 16 ranges: 32.6 us
-// and 23.1, replayed; 8 heads, 4 rows, 2400 keys in 10: 10.7 and 10.4.)
+// What adding up the ranges of a launch costs: by the block that finishes last (bytes: of a row tile) or in a launch of its
+// own, which reads with all compute units but costs a caller without a graph another 4 us of host time.  (1 head, 108 rows,
+// 21419 keys in 16 ranges: 32.6 us and 23.1, replayed; 8 heads, 4 rows, 2400 keys in 10: 10.7 and 10.4.)
 inline float join_last(float bytes) { return 3.2f + bytes / 18900.f; }
 inline float join_launch(float bytes) { return 6.f + bytes / 3090000.f; }
 
 // The shape and the number of ranges whose estimate is least: rounds of a block, each as long as a compute unit takes with the
-// blocks that fall to it, or what the memory takes for the keys and values, a fixed cost for every block of a compute unit, and the joining.  Blocks of
-// a chunk longer than any tree see half of the new keys on average, and as they are of all lengths, the longest first, they fill the chip
-// more evenly.  The choices take 1.02 times the best measured one over the inputs above, one in thirty of
-// them more than 1.15 times, at worst 1.29; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8 times that.
+// blocks that fall to it, or what the memory takes for the keys and values, a fixed cost for every block of a compute unit, and
+// the joining.  Blocks of a chunk longer than any tree see half of the new keys on average, and as they are of all lengths, the
+// longest first, they fill the chip more evenly.  The choices take 1.02 times the best measured one over the inputs above, one
+// in thirty of them more than 1.15 times, at worst 1.29; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8
+// times that.
 PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64_t S) {
   PagedPlan p{};
   const int64_t R = M * gq, heads = B * cache->Hkv;
@@ -1053,9 +1063,10 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   a.rc_gq = reciprocal((uint32_t)gq, (uint64_t)M * gq);
   a.table_stride = table_stride; a.page_shift = cache->page_shift; a.n_pages = cache->n_pages;
   a.row_blocks = p.row_blocks; a.nsplit = p.nsplit; a.range = p.range;
-  // Lengths are looked at where blocks are long enough to pay for it (half a microsecond each): ranges of three rounds or more in
-  // launches of up to two blocks a compute unit, which shorter ranges fill better (3 items, 48 heads over 12 of 128, 277 rows, 708 to 2124
-  // keys, 972 blocks: 73 us, 86 with shorter ones); without ranges, eight rounds or more in launches that do not fit at once.
+  // Lengths are looked at where blocks are long enough to pay for it (half a microsecond each): ranges of three rounds or more
+  // in launches of up to two blocks a compute unit, which shorter ranges fill better (3 items, 48 heads over 12 of 128, 277
+  // rows, 708 to 2124 keys, 972 blocks: 73 us, 86 with shorter ones); without ranges, eight rounds or more in launches that do
+  // not fit at once.
   const int64_t blocks = units * p.row_blocks, n_cu = cache->n_cu;
   const int per = p.range / p.wk;
   a.share = B > 1 && B <= 64 && (seq_len || row_len) && (p.nsplit > 1 ? per >= 3 && blocks <= 2 * n_cu : per >= 8 && blocks > n_cu) ? B : 0;

@@ -7,10 +7,11 @@
 // theta_j comes from the handle in turns per position, float64: p theta_j is formed in float64 and only its fraction of a
 // turn is rounded to float32, so that far positions (2^20 and more) turn as exactly as near ones.
 //
-// Bound by memory: every number is read and written once, and the layout changes from rows of heads to heads of rows on the way.
-// A lane has 8 pairs of one row (two 16-byte pieces of bf16) and goes through a group of heads with the same cosines and sines.  (4 chunks of up to
-// 2048 rows, 32 heads and 8 of 128 in bf16: 29.4 us, 4.3 TB/s of the 4.95 that a copy reaches; groups of all heads, fewer blocks than the chip
-// holds, 36.7 us; one of a verification step's 61 rows, 72 heads in all: 4.1 us and 5.9.)
+// Bound by memory: every number is read and written once, and the layout changes from rows of heads to heads of rows on the
+// way. A lane has 8 pairs of one row (two 16-byte pieces of bf16) and goes through a group of heads with the same cosines and
+// sines.  (4 chunks of up to 2048 rows, 32 heads and 8 of 128 in bf16: 29.4 us, 4.3 TB/s of the 4.95 that a copy reaches;
+// groups of all heads, fewer blocks than the chip holds, 36.7 us; one of a verification step's 61 rows, 72 heads in all: 4.1 us
+// and 5.9.)
 #include <math.h>
 
 #include <algorithm>
