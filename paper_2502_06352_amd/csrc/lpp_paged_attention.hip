@@ -934,8 +934,8 @@ inline float join_launch(float bytes) { return 6.f + bytes / 3090000.f; }
 // blocks that fall to it, or what the memory takes for the keys and values, a fixed cost for every block of a compute unit, and
 // the joining.  Blocks of a chunk longer than any tree see half of the new keys on average, and as they are of all lengths, the
 // longest first, they fill the chip more evenly.  The choices take 1.02 times the best measured one over the inputs above, one
-// in thirty of them more than 1.15 times, at worst 1.29; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8
-// times that.
+// in thirty of them more than 1.15 times, at worst 1.29, and 1.05 times over 80 others of few rows and long caches, at worst
+// 1.38; blocks of 32, 64 or 128 rows by the number of rows alone took up to 8 times that.
 PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64_t S) {
   PagedPlan p{};
   const int64_t R = M * gq, heads = B * cache->Hkv;

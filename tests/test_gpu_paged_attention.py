@@ -317,3 +317,50 @@ def test_tensors_of_the_host_are_refused():
             c.call(t)
         assert e.value.status == lpp.LPP_EINVAL
     c.run()
+
+
+def test_two_graphs_share_a_handle_and_a_workspace():
+    """Captured one after the other, replayed in turn on one stream, with eager calls on the same handle in between."""
+    cases = [Case(3, 8, 2, 128, 16, [3000, 40, 1700], parent=TINY, seed=34), Case(2, 8, 2, 128, 16, [90, 5000], M=70, rows=[70, 31], seed=35)]
+    n_pages, states = max(c.n_pages for c in cases), [c.upload() for c in cases]
+    ws = torch.full((max(t["ws"].numel() for t in states),), 255, dtype=torch.uint8, device=DEV)
+    cache = lpp.PagedCache(lpp.LPP_BF16, 2, 128, 16, n_pages)
+    for c, t in zip(cases, states):
+        assert t["ws"].numel() > 256
+        t["kp"], t["vp"] = (torch.cat([x, x.new_zeros(n_pages - c.n_pages, 2, 16, 128)]) for x in (t["kp"], t["vp"]))
+        t.update(ws=ws, cache=cache)
+    eager = [c.call(t).clone() for c, t in zip(cases, states)]
+    for c, out in zip(cases, eager):
+        c.check(out)
+    side, graphs = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for c, t in zip(cases, states):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graphs[-1], stream=side):
+                c.call(t, side)
+    for which in (0, 1, 1, 0, 1, 0):
+        states[which]["out"].fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[which].replay()
+            other = states[1 - which]
+            other["out"].fill_(7.0)
+            cases[1 - which].call(other, side)
+        side.synchronize()
+        assert torch.equal(states[which]["out"], eager[which]) and torch.equal(other["out"], eager[1 - which])
+
+
+def test_two_streams_with_a_handle_each():
+    """Calls that may overlap: what they leave in their handles and workspaces is their own."""
+    cases = [Case(2, 8, 2, 128, 16, [4000, 2500], parent=TINY, seed=s) for s in (36, 37)]
+    states, streams = [c.upload() for c in cases], [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = [c.call(t).clone() for c, t in zip(cases, states)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, t, s in zip(cases, states, streams):
+            c.call(t, s)
+    torch.cuda.synchronize()
+    for c, t, w in zip(cases, states, want):
+        assert torch.equal(t["out"], w)
+        c.check(w)
