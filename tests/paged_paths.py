@@ -1,0 +1,37 @@
+"""Inputs of paged attention by the path that their plan takes: tests/test_paged_plan.py holds them to it (no GPU), and
+tests/test_gpu_paged_paths.py runs them.
+
+dtype, Dh, the shape of a block, how a row's ranges of keys are joined ("one": there is one; "last": by the block that finishes
+last; "later": in a launch of their own), whether blocks look at all items' lengths, form, B, H, Hkv, M, S, page size."""
+
+# what the blocks of a row tile leave in the handle for each other is back to zero behind the call
+JOINED_BY_THE_LAST_BLOCK = [
+    ("bf16", 64, 0, "last", 0, "chunk", 3, 3, 3, 1, 6807, 32),
+    ("bf16", 64, 0, "last", 1, "tree", 7, 3, 3, 1, 5909, 64),
+    ("bf16", 64, 1, "last", 0, "tree", 3, 4, 4, 1, 5364, 32),
+    ("bf16", 64, 1, "last", 1, "chunk", 11, 2, 2, 1, 5861, 64),
+    ("bf16", 64, 2, "last", 0, "tree", 1, 96, 24, 61, 3070, 64),
+    ("bf16", 64, 2, "last", 1, "chunk", 34, 1, 1, 33, 1479, 128),
+    ("bf16", 128, 0, "last", 0, "tree", 3, 3, 3, 1, 5516, 256),
+    ("bf16", 128, 0, "last", 1, "chunk", 2, 8, 8, 1, 6163, 16),
+    ("bf16", 128, 1, "last", 0, "chunk", 10, 1, 1, 1, 6704, 256),
+    ("bf16", 128, 1, "last", 1, "tree", 8, 2, 2, 1, 6781, 16),
+    ("bf16", 128, 2, "last", 0, "chunk", 1, 32, 16, 130, 1659, 16),
+    ("bf16", 128, 2, "last", 1, "tree", 17, 12, 4, 16, 1551, 32),
+    ("bf16", 128, 3, "last", 0, "chunk", 1, 96, 24, 199, 2042, 32),
+    ("bf16", 128, 3, "last", 1, "tree", 18, 6, 3, 129, 1918, 64),
+    ("bf16", 128, 4, "last", 1, "chunk", 5, 32, 16, 33, 3546, 64),
+    ("f32", 64, 0, "last", 0, "tree", 6, 2, 2, 1, 5408, 64),
+    ("f32", 64, 0, "last", 1, "chunk", 9, 3, 3, 1, 4901, 128),
+    ("f32", 64, 1, "last", 0, "chunk", 9, 9, 3, 6, 1187, 64),
+    ("f32", 64, 1, "last", 1, "tree", 6, 2, 2, 129, 883, 128),
+    ("f32", 128, 0, "last", 0, "chunk", 6, 1, 1, 1, 5385, 128),
+    ("f32", 128, 0, "last", 1, "tree", 6, 2, 2, 1, 5425, 256),
+    ("f32", 128, 1, "last", 0, "chunk", 2, 24, 24, 17, 748, 256),
+    ("f32", 128, 1, "last", 1, "tree", 5, 2, 2, 129, 1138, 16),
+]
+
+# lengths of batches of single tokens, 8 heads over 2 of 128
+TOKENS = [[3000], [1500, 2900]]
+
+PATHS = JOINED_BY_THE_LAST_BLOCK

@@ -1,0 +1,85 @@
+"""GPU: paged attention on every path that a plan may take (tests/paged_paths.py), against the oracle.  Tolerances are those of
+test_gpu_paged_attention."""
+import numpy as np
+import pytest
+import torch
+
+import paged_paths
+from gpu_common import DEV
+from test_gpu_paged_attention import TINY, WIDE, XXL, Case
+import paper_2502_06352_amd as lpp
+
+pytestmark = pytest.mark.gpu
+
+PARENTS = {1: [-1], 16: TINY, 61: XXL, 129: WIDE}
+
+
+def _case(path, seed):
+    """Items of all lengths, the longest neither first nor last, ties, empty ones and ones without rows among them; where there are
+    rows enough an infinity and a NaN among the new values, and a new key of NaN that its own row alone sees."""
+    dtype, Dh, _, _, _, form, B, H, Hkv, M, S, page = path
+    lens = np.random.default_rng(seed).integers(0, S + 1, B)
+    lens[B // 2] = S
+    if B > 2:
+        lens[0], lens[-1] = 0, lens[1]
+    if form == "tree":
+        c = Case(B, H, Hkv, Dh, page, lens.tolist(), parent=PARENTS[M], S=S, dtype=dtype, seed=seed)
+    else:
+        rows = [(M, M - 1, M // 2 + 1, M + 5, 1, 0, -3)[(b - B // 2) % 7] for b in range(B)]
+        c = Case(B, H, Hkv, Dh, page, lens.tolist(), M=M, rows=rows, S=S, dtype=dtype, seed=seed)
+    if M > 4:
+        b = B // 2                                         # (has all M rows)
+        c.vn[b, 0, 2 * M // 3, 3], c.vn[b, Hkv - 1, M - 2, Dh - 1] = np.inf, np.nan
+        c.kn[b, 0, M - 1, 5] = np.nan
+    return c
+
+
+def _bits(t):
+    return t.view(torch.int16 if t.dtype is torch.bfloat16 else torch.int32)
+
+
+@pytest.mark.parametrize("i", range(len(paged_paths.PATHS)))
+def test_paths(i):
+    """Three calls on one handle and workspace, the outputs filled anew: the oracle's result, and the same bits each time."""
+    path = paged_paths.PATHS[i]
+    print(path, flush=True)
+    c = _case(path, seed=100 + i)
+    t = c.upload()
+    first = c.call(t).clone()
+    c.check(first)
+    for _ in range(2):
+        t["out"].fill_(7.0)
+        t["ws"].fill_(255)
+        assert torch.equal(_bits(c.call(t)), _bits(first))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_calls_that_the_last_block_joins(dtype):
+    """Two graphs on one handle and workspace, replayed in turn with eager calls in between."""
+    cases = [Case(len(lens), 8, 2, 128, 16, lens, parent=[-1], dtype=dtype, seed=60 + i) for i, lens in enumerate(paged_paths.TOKENS)]
+    n_pages, states = max(c.n_pages for c in cases), [c.upload() for c in cases]
+    ws = torch.full((max(t["ws"].numel() for t in states),), 255, dtype=torch.uint8, device=DEV)
+    cache = lpp.PagedCache(states[0]["cache"].dtype, 2, 128, 16, n_pages)
+    for c, t in zip(cases, states):
+        t["kp"], t["vp"] = (torch.cat([x, x.new_zeros(n_pages - c.n_pages, 2, 16, 128)]) for x in (t["kp"], t["vp"]))
+        t.update(ws=ws, cache=cache)
+    eager = [c.call(t).clone() for c, t in zip(cases, states)]
+    for c, out in zip(cases, eager):
+        c.check(out)
+    side, graphs = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for c, t in zip(cases, states):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graphs[-1], stream=side):
+                c.call(t, side)
+    for which in (0, 1, 1, 0, 0):
+        for t in states:
+            t["out"].fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[which].replay()
+            cases[1 - which].call(states[1 - which], side)
+        side.synchronize()
+        for t, want in zip(states, eager):
+            assert torch.equal(t["out"], want)
