@@ -31,7 +31,24 @@ JOINED_BY_THE_LAST_BLOCK = [
     ("f32", 128, 1, "last", 1, "tree", 5, 2, 2, 129, 1138, 16),
 ]
 
+# one range: which item a block takes goes by the lengths
+LONGEST_FIRST = [
+    ("bf16", 64, 0, "one", 1, "chunk", 11, 24, 24, 1, 929, 16),
+    ("bf16", 64, 1, "one", 1, "chunk", 17, 24, 8, 11, 1858, 32),
+    ("bf16", 64, 2, "one", 1, "chunk", 35, 24, 8, 11, 898, 64),
+    ("bf16", 64, 3, "one", 1, "chunk", 23, 32, 16, 36, 471, 256),
+    ("bf16", 64, 4, "one", 1, "chunk", 34, 32, 8, 25, 650, 128),
+    ("bf16", 128, 1, "one", 1, "tree", 30, 3, 3, 129, 1663, 256),
+    ("bf16", 128, 2, "one", 1, "tree", 34, 24, 8, 16, 886, 16),
+    ("bf16", 128, 3, "one", 1, "tree", 22, 8, 8, 129, 265, 32),
+    ("bf16", 128, 4, "one", 1, "chunk", 38, 3, 3, 257, 214, 32),
+    ("f32", 64, 0, "one", 1, "tree", 34, 12, 4, 16, 1848, 32),
+    ("f32", 64, 1, "one", 1, "tree", 29, 3, 3, 129, 753, 64),
+    ("f32", 128, 0, "one", 1, "tree", 43, 9, 3, 16, 903, 128),
+    ("f32", 128, 1, "one", 1, "tree", 11, 8, 8, 129, 806, 256),
+]
+
 # lengths of batches of single tokens, 8 heads over 2 of 128
 TOKENS = [[3000], [1500, 2900]]
 
-PATHS = JOINED_BY_THE_LAST_BLOCK
+PATHS = JOINED_BY_THE_LAST_BLOCK + LONGEST_FIRST
