@@ -48,7 +48,49 @@ LONGEST_FIRST = [
     ("f32", 128, 1, "one", 1, "tree", 11, 8, 8, 129, 806, 256),
 ]
 
+# every other shape with every way of joining that it is chosen with
+OTHERS = [
+    ("bf16", 64, 0, "later", 0, "chunk", 3, 6, 3, 7, 6972, 128),
+    ("bf16", 64, 0, "one", 0, "tree", 17, 16, 16, 1, 258, 256),
+    ("bf16", 64, 1, "later", 0, "tree", 5, 2, 2, 16, 6640, 128),
+    ("bf16", 64, 1, "later", 1, "chunk", 5, 4, 4, 29, 6383, 256),
+    ("bf16", 64, 1, "one", 0, "tree", 1, 1, 1, 1, 228, 16),
+    ("bf16", 64, 2, "later", 0, "tree", 5, 3, 1, 16, 6507, 256),
+    ("bf16", 64, 2, "later", 1, "chunk", 4, 9, 3, 11, 5554, 16),
+    ("bf16", 64, 2, "one", 0, "tree", 43, 9, 3, 16, 220, 32),
+    ("bf16", 64, 3, "one", 0, "tree", 28, 8, 8, 129, 240, 128),
+    ("bf16", 64, 4, "later", 0, "chunk", 2, 4, 2, 34, 5471, 16),
+    ("bf16", 64, 4, "later", 1, "chunk", 4, 4, 2, 33, 5592, 32),
+    ("bf16", 64, 4, "one", 0, "tree", 27, 12, 4, 61, 200, 64),
+    ("bf16", 128, 0, "later", 0, "tree", 4, 2, 2, 16, 6142, 32),
+    ("bf16", 128, 0, "later", 1, "chunk", 2, 8, 8, 11, 6180, 64),
+    ("bf16", 128, 0, "one", 0, "tree", 30, 8, 8, 1, 210, 128),
+    ("bf16", 128, 1, "later", 0, "chunk", 10, 1, 1, 8, 6625, 32),
+    ("bf16", 128, 1, "later", 1, "tree", 2, 8, 8, 16, 6776, 64),
+    ("bf16", 128, 1, "one", 0, "chunk", 1, 1, 1, 1, 330, 128),
+    ("bf16", 128, 2, "later", 0, "chunk", 7, 3, 1, 11, 4942, 64),
+    ("bf16", 128, 2, "later", 1, "tree", 3, 12, 4, 16, 5242, 128),
+    ("bf16", 128, 2, "one", 0, "chunk", 34, 16, 4, 9, 222, 256),
+    ("bf16", 128, 3, "later", 0, "chunk", 1, 96, 24, 18, 6267, 128),
+    ("bf16", 128, 3, "later", 1, "tree", 15, 6, 3, 61, 4062, 256),
+    ("bf16", 128, 3, "one", 0, "chunk", 11, 72, 24, 23, 291, 16),
+    ("bf16", 128, 4, "later", 0, "tree", 1, 48, 24, 61, 3540, 128),
+    ("bf16", 128, 4, "later", 1, "chunk", 4, 8, 4, 34, 2046, 256),
+    ("bf16", 128, 4, "one", 0, "tree", 44, 2, 2, 129, 203, 16),
+    ("f32", 64, 0, "later", 0, "tree", 4, 3, 3, 16, 6667, 256),
+    ("f32", 64, 0, "one", 0, "chunk", 1, 4, 1, 1, 243, 16),
+    ("f32", 64, 1, "later", 0, "chunk", 2, 9, 3, 6, 5637, 256),
+    ("f32", 64, 1, "later", 1, "tree", 11, 1, 1, 61, 3841, 16),
+    ("f32", 64, 1, "one", 0, "chunk", 45, 3, 3, 17, 100, 32),
+    ("f32", 128, 0, "later", 0, "chunk", 5, 4, 1, 1, 6733, 16),
+    ("f32", 128, 0, "later", 1, "tree", 2, 1, 1, 129, 3491, 32),
+    ("f32", 128, 0, "one", 0, "chunk", 1, 1, 1, 1, 114, 64),
+    ("f32", 128, 1, "later", 0, "chunk", 1, 8, 8, 17, 6189, 32),
+    ("f32", 128, 1, "later", 1, "tree", 6, 1, 1, 61, 5332, 64),
+    ("f32", 128, 1, "one", 0, "chunk", 33, 12, 4, 6, 197, 128),
+]
+
 # lengths of batches of single tokens, 8 heads over 2 of 128
 TOKENS = [[3000], [1500, 2900]]
 
-PATHS = JOINED_BY_THE_LAST_BLOCK + LONGEST_FIRST
+PATHS = JOINED_BY_THE_LAST_BLOCK + LONGEST_FIRST + OTHERS
