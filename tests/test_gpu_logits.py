@@ -137,3 +137,15 @@ def test_commit_counts():
         for x in tokens[b, 1:1 + accept[b]].clip(0, V - 1).tolist() + [int(final[b])]:
             want[b, x] += 1
     assert np.array_equal(counts.cpu().numpy(), want)
+
+
+WIDE = static_tree((8, 4, 2, 2, 1, 1, 1, 1), 128)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(guided=True), dict(dtype="bf16"), dict(dtype="bf16", guided=True, bias=2, mask=2),
+                                dict(in_place=True, guided=True, few=True)])
+def test_many_rows(kw):
+    """4 x 129 rows in pieces of 2048 tokens, the last of one token: blocks of two groups of four tokens a lane, which are taken where
+    they are four a compute unit (here 1548 blocks)."""
+    assert 4 * 129 * 3 >= 4 * torch.cuda.get_device_properties(0).multi_processor_count
+    _run(WIDE, 4, 4097, 5, 3, seed=7, **kw)
