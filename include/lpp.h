@@ -415,7 +415,9 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  *             above the lengths costs time.  S = 0: nothing is cached, pages and table may be NULL.  table_stride * page_size >= S
  *   seq_len   [device] int32 [B] or NULL (= S);  row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M)
  *   scale     0 selects 1/sqrt(Dh); negative, infinite or NaN is LPP_EINVAL
- *   ws        lpp_paged_attention_workspace(cache, B, H, M, S) bytes
+ *   ws        lpp_paged_attention_workspace(cache, B, H, M, S) bytes, a number that grows with all four: a workspace made for the
+ *             largest sizes serves every call of no more items, heads, rows and positions on a handle of the same geometry.  At most 768 rows of
+ *             Dh + 2 floats a compute unit (102 MB for Dh 128)
  * Softmax and accumulation are float32; bf16 products run on the bf16 matrix cores with the weights rounded to bf16.  What a row
  * does not see plays no part in it, whatever it holds.  Scores (scale times the product) are to stay below 10^29 in
  * magnitude.  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments

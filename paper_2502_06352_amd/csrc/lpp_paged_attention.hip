@@ -968,7 +968,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   const PagedPlan p = plan_paged(cache, B, gq, M, S);
   const int64_t units = (int64_t)B * cache->Hkv * p.nsplit;
   if (units * p.row_blocks >= (1ll << 31)) return LPP_EUNSUPPORTED;
-  if (p.o_bytes + p.ml_bytes > 0 && (!ws || misaligned(ws) || ws_bytes < p.o_bytes + p.ml_bytes)) return LPP_ENOWORKSPACE;
+  if (p.o_bytes > 0 && (!ws || misaligned(ws) || ws_bytes < paged_room(cache, B, gq, M, S))) return LPP_ENOWORKSPACE;
   if (!cache->d_counters || (tree && !tree->d_anc)) return LPP_EHIP;     // host-only handle: no device
   if (!lpp_is_current(cache->device) || (tree && tree->device != cache->device)) return LPP_EINVAL;
   if (scale == 0.f) scale = 1.0f / sqrtf((float)cache->Dh);
@@ -996,8 +996,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
 
 extern "C" size_t lpp_paged_attention_workspace(const lpp_paged* cache, int32_t B, int32_t H, int32_t M, int32_t S) {
   if (!cache || B < 1 || H < 1 || M < 1 || S < 0 || H % cache->Hkv != 0) return 0;
-  const PagedPlan p = plan_paged(cache, B, H / cache->Hkv, M, S);
-  return std::max<size_t>(p.o_bytes + p.ml_bytes, 256);
+  return std::max<size_t>(paged_room(cache, B, H / cache->Hkv, M, S), 256);
 }
 
 extern "C" int32_t lpp_paged_tree_attention(const lpp_paged* cache, const lpp_tree* tree, const void* q, const void* k_pages,

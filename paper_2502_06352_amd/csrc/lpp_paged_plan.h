@@ -16,7 +16,11 @@ struct PagedPlan {
   int row_blocks, nsplit, range;
   bool join_later;
   size_t lds;
-  size_t o_bytes, ml_bytes;          // partials
+  size_t o_bytes, ml_bytes;          // parts of rows: numbers, references and sums
+  void room_for(int64_t part_rows, int Dh) {
+    o_bytes = lpp_align_up((size_t)part_rows * Dh * sizeof(float), 256);
+    ml_bytes = lpp_align_up((size_t)part_rows * 2 * sizeof(float), 256);
+  }
 };
 
 // Shapes of a bf16 block, and what a round of its waves (kt * wk keys) costs in microseconds: with heads of 64 and of 128
@@ -32,6 +36,43 @@ constexpr Shape kShapes[] = {
     {4, 2, 32, 2, {2, 1}, {0.74f, 0.76f}, {0.58f, 1.14f}},
 };
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+constexpr int kMostRanges = 128;
+// (float32: the second row is of two tiles of 16 rows)
+inline Shape shape_of(const lpp_paged* cache, int i) {
+  if (cache->dtype == LPP_BF16) return kShapes[i];
+  if (i == 0) return {1, cache->Dh == 64 ? 16 : 8, 16, 0, {1, 1}, {3.3f, 3.2f}, {3.1f, 3.2f}};
+  return {2, 8, 16, 0, {1, 1}, {3.0f, 5.2f}, {2.9f, 5.5f}};
+}
+inline int shapes(const lpp_paged* cache) { return cache->dtype == LPP_BF16 ? (int)(sizeof(kShapes) / sizeof(kShapes[0])) : 2; }
+inline int rows_of(const lpp_paged* cache, const Shape& h) { return h.wr * (cache->dtype == LPP_BF16 ? 32 : 16); }
+// Whether blocks of shape i are for R rows: no block has more rows than the next smaller one would.
+inline bool fits_rows(int i, const Shape& h, int rows, int64_t R) { return i == 0 || h.wr == 1 || R > rows / 2; }
+inline int64_t rounds_of(const Shape& h, int64_t M, int64_t S) {
+  return ((S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt + h.wk - 1) / h.wk;
+}
+
+// Rows of parts that a launch has at most: 6 blocks of the largest shape a compute unit (102 MB with heads of 128 numbers).  Without a
+// limit batches that fill the chip many times over are cut in two for a percent or two, by the estimate, and up to gigabytes
+// of parts.  (56 calls that limits of 512, 768 or 1024 rows concern, 100 to 600 us: 0.95, 0.94 and 0.97 of the time without, at worst
+// 1.16, 1.13 and 1.04; 100 items of 123 rows, 16 heads over 8 of 128, up to 4161 keys: 469 us without, 287 with.)
+inline int64_t most_part_rows(const lpp_paged* cache) { return (int64_t)cache->n_cu * 768; }
+
+// Room for the parts of every call of up to B items, M rows of gq heads and S positions: whatever shape and number of ranges each of
+// them is cut into.  It grows with all of these, so that a caller may make its workspace once.
+inline size_t paged_room(const lpp_paged* cache, int64_t B, int gq, int64_t M, int64_t S) {
+  const int64_t R = M * gq, heads = B * cache->Hkv;
+  int64_t most = 0;
+  for (int i = 0; i < shapes(cache); ++i) {
+    const Shape h = shape_of(cache, i);
+    const int rows = rows_of(cache, h);
+    if (!fits_rows(i, h, rows, R)) break;
+    const int64_t rounds = rounds_of(h, M, S), units = heads * ((R + rows - 1) / rows);
+    if (rounds > 1) most = std::max(most, std::min(units * std::min<int64_t>(rounds, kMostRanges) * rows, most_part_rows(cache)));
+  }
+  PagedPlan p{};
+  p.room_for(most, cache->Dh);
+  return p.o_bytes + p.ml_bytes;
+}
 
 // What adding up the ranges of a launch costs: by the block that finishes last (bytes: of a row tile) or in a launch of its
 // own, which reads with all compute units but costs a caller without a graph another 4 us of host time.  (1 head, 108 rows,
@@ -50,15 +91,14 @@ inline PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M
   const int64_t R = M * gq, heads = B * cache->Hkv;
   const int Dh = cache->Dh, d = Dh == 128;
   const bool bf16 = cache->dtype == LPP_BF16;
-  const Shape f32[2] = {{1, Dh == 64 ? 16 : 8, 16, 0, {1, 1}, {3.3f, 3.2f}, {3.1f, 3.2f}}, {2, 8, 16, 0, {1, 1}, {3.0f, 5.2f}, {2.9f, 5.5f}}};
   float best = INFINITY;
   const float memory = (float)heads * (float)(S + M) * (float)(Dh * (bf16 ? 4 : 8)) / 9.e6f;   // (two thirds of the inputs were shorter than S)
-  for (int i = 0; i < (bf16 ? (int)(sizeof(kShapes) / sizeof(kShapes[0])) : 2); ++i) {
-    const Shape& h = bf16 ? kShapes[i] : f32[i];
-    const int rows = h.wr * (bf16 ? 32 : 16);
-    if (i > 0 && h.wr > 1 && R <= rows / 2) break;   // (no block has more rows than the next smaller one would)
+  for (int i = 0; i < shapes(cache); ++i) {
+    const Shape h = shape_of(cache, i);
+    const int rows = rows_of(cache, h);
+    if (!fits_rows(i, h, rows, R)) break;
     const int64_t row_blocks = (R + rows - 1) / rows, units = heads * row_blocks;
-    const int tiles = (int)((S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt), rounds = (tiles + h.wk - 1) / h.wk;
+    const int tiles = (int)((S + h.kt - 1) / h.kt + (M + h.kt - 1) / h.kt), rounds = (int)rounds_of(h, M, S);
     const bool causal = M > LPP_MAX_ROWS;
     const float seen = causal ? 1.f - 0.5f * (float)((M + h.kt - 1) / h.kt) / (float)tiles : 1.f, full = causal ? 0.35f : 0.75f;
     int before = 0;
@@ -67,7 +107,7 @@ inline PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M
       if (ranges == before) continue;                // (as many as the last choice)
       before = ranges;
       const int64_t blocks = units * ranges;
-      if (ranges > 1 && blocks * rows * (Dh + 2) * 4 >= (int64_t)1 << 31) break;      // (32-bit offsets into the parts)
+      if (ranges > 1 && blocks * rows > most_part_rows(cache)) break;                 // (32-bit offsets into the parts, too)
       const float each = (float)blocks / (float)cache->n_cu, k = ceilf(each);
       const float load = (1.f - full) * std::max(1.f, each * seen) + full * k * seen;      // (between the average and the fullest)
       const float turns = 1.f + (ceilf(k / (float)h.resident[d]) - 1.f) * seen;
@@ -89,9 +129,7 @@ inline PagedPlan plan_paged(const lpp_paged* cache, int64_t B, int gq, int64_t M
       if (per == 1 || (ranges > 1 && each > 8.f)) break;
     }
   }
-  const size_t parts = p.nsplit > 1 ? (size_t)heads * p.row_blocks * p.nsplit * p.rows : 0;
-  p.o_bytes = lpp_align_up(parts * Dh * sizeof(float), 256);
-  p.ml_bytes = lpp_align_up(parts * 2 * sizeof(float), 256);
+  p.room_for(p.nsplit > 1 ? heads * p.row_blocks * p.nsplit * p.rows : 0, Dh);
   return p;
 }
 

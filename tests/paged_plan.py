@@ -16,6 +16,11 @@ extern "C" void plan(int32_t bf16, int32_t Hkv, int32_t Dh, int32_t n_cu, int64_
                         (int64_t)(p.o_bytes + p.ml_bytes)};
   for (int64_t x : of) *out++ = x;
 }
+extern "C" int64_t room(int32_t bf16, int32_t Hkv, int32_t Dh, int32_t n_cu, int64_t B, int32_t gq, int64_t M, int64_t S) {
+  lpp_paged c;
+  c.dtype = bf16 ? LPP_BF16 : LPP_F32; c.Hkv = Hkv; c.Dh = Dh; c.n_cu = n_cu;
+  return (int64_t)paged_room(&c, B, gq, M, S);
+}
 """
 Plan = namedtuple("Plan", "shape rows kt wk row_blocks nsplit range join_later by_lengths bytes")
 
@@ -28,9 +33,15 @@ def build(folder):
     L = C.CDLL(str(folder / "t.so"))
     L.plan.argtypes, L.plan.restype = [C.c_int32] * 4 + [C.c_int64, C.c_int32, C.c_int64, C.c_int64, C.c_void_p], None
 
+    L.room.argtypes, L.room.restype = [C.c_int32] * 4 + [C.c_int64, C.c_int32, C.c_int64, C.c_int64], C.c_int64
+
     def plan(dtype, B, H, Hkv, Dh, M, S, n_cu=256):
         out = (C.c_int64 * len(Plan._fields))()
         L.plan(dtype == "bf16", Hkv, Dh, n_cu, B, H // Hkv, M, S, out)
         return Plan(*out)
 
+    def room(dtype, B, H, Hkv, Dh, M, S, n_cu=256):
+        return L.room(dtype == "bf16", Hkv, Dh, n_cu, B, H // Hkv, M, S)
+
+    plan.room = room
     return plan

@@ -83,3 +83,22 @@ def test_captured_calls_that_the_last_block_joins(dtype):
         side.synchronize()
         for t, want in zip(states, eager):
             assert torch.equal(t["out"], want)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,Dh,largest,calls", [
+    ("bf16", 32, 8, 128, (64, 1, 900), [(64, 900), (1, 900), (3, 700), (2, 0), (64, 31)]),
+    ("f32", 16, 16, 64, (60, 16, 700), [(2, 600), (60, 700), (1, 699)])])
+def test_one_workspace_for_calls_of_all_sizes(dtype, H, Hkv, Dh, largest, calls):
+    """Made for the largest batch; smaller ones are cut into more ranges.  Nothing is written behind it."""
+    B, M, S = largest
+    parent = PARENTS[M]
+    cache = lpp.PagedCache(lpp.LPP_BF16 if dtype == "bf16" else lpp.LPP_F32, Hkv, Dh, 32, 1)
+    n = lpp.lpp_paged_attention_workspace(cache, B, H, M, S)
+    whole = torch.full((n + 4096,), 165, dtype=torch.uint8, device=DEV)
+    for i, (items, most) in enumerate(calls):
+        lens = [most * (b + 1) // items for b in range(items)]
+        c = Case(items, H, Hkv, Dh, 32, lens, parent=parent, dtype=dtype, seed=70 + i)
+        t = c.upload()
+        t["ws"] = whole[:n]
+        c.check(c.call(t))
+        assert bool((whole[n:] == 165).all())

@@ -236,3 +236,19 @@ def test_the_binding_refuses_tensors_of_other_sizes_types_and_strides():
     for bad in (dict(x=x[:, :2]), dict(out=x.bfloat16()), dict(tokens=torch.zeros(B, M)), dict(counts=torch.zeros(B, 39, **i32)),
                 dict(repetition=one[:1]), dict(bias=torch.zeros(39)), dict(mask=torch.zeros(B, M, 1, **i32))):
         assert logits(**bad) == EINVAL, bad
+
+
+@no_gpu
+def test_a_workspace_serves_smaller_calls(L):
+    """Two items of 512 rows over up to 3264 positions, then less of each: more ranges of keys, in the same workspace."""
+    cache = lpp.PagedCache(lpp.LPP_BF16, 8, 128, 16, 4)
+    n = lpp.lpp_paged_attention_workspace(cache, 2, 32, 512, 3264)
+
+    def chunk(B, M, S, n):
+        return L.lpp_paged_chunk_attention(cache.handle, FAKE, FAKE, FAKE, FAKE, 204, FAKE, FAKE, None, None, B, 32, M, S, 0.0, 2 * FAKE, FAKE, n,
+                                           None)
+
+    for B, M, S in ((2, 512, 3200), (1, 512, 3264), (1, 1, 3264), (2, 100, 2000), (1, 40, 900), (2, 512, 3264)):
+        assert lpp.lpp_paged_attention_workspace(cache, B, 32, M, S) <= n
+        assert chunk(B, M, S, n) == EHIP
+    assert chunk(1, 1, 3264, lpp.lpp_paged_attention_workspace(cache, 1, 32, 1, 3264) - 1) == lpp.LPP_ENOWORKSPACE
