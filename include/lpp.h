@@ -456,9 +456,9 @@ int32_t lpp_paged_chunk_attention(const lpp_paged* cache, const void* q, const v
  *   first_pos           [device] int32 [B] or NULL (= 0);  row_len [device] int32 [B] or NULL: rows behind an item's
  *                       last are not written
  *   q_out [B, H, M, Dh], k_out and v_out [B, Hkv, M, Dh]   [device] contiguous, 16-byte aligned; an output may be its input
- *                       if the strides are the output's, and must not overlap one otherwise
+ *                       if the strides are the output's, and must overlap no input otherwise, nor another output
  * The handle lives on the host (it may be used on any device).  Errors: LPP_EINVAL (null, sizes < 1, tree of another M, dim > Dh,
- * an unknown enumerator, a config out of range, misaligned or partly overlapping in place), LPP_EUNSUPPORTED (dtype, dim or Dh not a multiple of
+ * an unknown enumerator, a config out of range, misaligned, outputs that overlap what they must not), LPP_EUNSUPPORTED (dtype, dim or Dh not a multiple of
  * 16 or too large, strides not multiples of 16 bytes), LPP_EHIP.
  */
 #define LPP_ROTARY_MAX_DIM     256

@@ -102,3 +102,18 @@ def test_one_workspace_for_calls_of_all_sizes(dtype, H, Hkv, Dh, largest, calls)
         t["ws"] = whole[:n]
         c.check(c.call(t))
         assert bool((whole[n:] == 165).all())
+
+
+def test_rotary_outputs_over_inputs_are_refused():
+    tree, rotary = lpp.Tree(TINY), lpp.Rotary(64)
+    B, M, H, Hkv, Dh = 2, 16, 4, 2, 64
+    qkv = torch.randn(B, M, H + 2 * Hkv, Dh, device=DEV)
+    q, k, v = qkv.split([H, Hkv, Hkv], 2)
+    outs = [torch.full((B, h, M, Dh), 7.0, device=DEV) for h in (H, Hkv, Hkv)]
+    over = qkv.view(-1)[H * Dh:H * Dh + B * H * M * Dh].view(B, H, M, Dh)
+    for bad in ((over, outs[1], outs[2]), (outs[0], outs[1], outs[1]), (outs[0], outs[0].view(-1)[:B * Hkv * M * Dh], outs[2])):
+        with pytest.raises(lpp.LppError) as e:
+            lpp.lpp_rotary_qkv(rotary, tree, lpp.LPP_F32, q, k, v, None, None, B, H, Hkv, M, Dh, *bad)
+        assert e.value.status == lpp.LPP_EINVAL
+    torch.cuda.synchronize()
+    assert all(bool((o == 7.0).all()) for o in outs)

@@ -252,3 +252,34 @@ def test_a_workspace_serves_smaller_calls(L):
         assert lpp.lpp_paged_attention_workspace(cache, B, 32, M, S) <= n
         assert chunk(B, M, S, n) == EHIP
     assert chunk(1, 1, 3264, lpp.lpp_paged_attention_workspace(cache, 1, 32, 1, 3264) - 1) == lpp.LPP_ENOWORKSPACE
+
+
+@no_gpu
+def test_rotary_refuses_outputs_over_inputs_and_each_other(L):
+    """A fused projection [B, M, H + 2 Hkv, Dh] in bf16 at `at`; without a tree, so that nothing but the launch is left."""
+    rotary = lpp.Rotary(64)
+    B, M, H, Hkv, Dh, at = 2, 5, 4, 2, 64, 1 << 20
+    item, row, width = M * (H + 2 * Hkv) * Dh, (H + 2 * Hkv) * Dh, 2 * Dh
+    end = at + B * item * 2
+
+    def call(qo=2 << 20, ko=3 << 20, vo=4 << 20, q=_rows(at, item, row, Dh), k=_rows(at + H * width, item, row, Dh),
+             v=_rows(at + (H + Hkv) * width, item, row, Dh), B=B, M=M):
+        return L.lpp_rotary_qkv(rotary.handle, None, lpp.LPP_BF16, q, k, v, None, None, B, H, Hkv, M, Dh, qo, ko, vo, None)
+
+    big, small = B * H * M * width, B * Hkv * M * width             # bytes of q_out, and of k_out and v_out
+    packed = _rows(2 << 20, H * M * Dh, Dh, M * Dh)
+    _refusals(call, {}, [
+        ({}, EHIP), (dict(qo=end), EHIP), (dict(qo=at - big), EHIP), (dict(vo=at - small), EHIP), (dict(ko=(2 << 20) + big), EHIP),
+        (dict(qo=at + H * width), EINVAL), (dict(qo=at + 16), EINVAL), (dict(qo=end - 16), EINVAL), (dict(qo=at - big + 16), EINVAL),
+        (dict(ko=at), EINVAL), (dict(vo=at + H * width), EINVAL), (dict(ko=end - 16), EINVAL), (dict(ko=end - small), EINVAL),
+        (dict(ko=2 << 20), EINVAL), (dict(vo=3 << 20), EINVAL), (dict(ko=(2 << 20) + big - 16), EINVAL), (dict(vo=(2 << 20) - small + 16), EINVAL),
+        # in place, and one's own neighbours
+        (dict(q=packed), EHIP), (dict(q=packed, ko=(2 << 20) + big - 16), EINVAL), (dict(q=packed, qo=(2 << 20) + 16), EINVAL),
+        # one row of one item is laid out as its output is: all three in place
+        (dict(B=1, M=1, qo=at, ko=at + H * width, vo=at + (H + Hkv) * width), EHIP),
+        (dict(B=1, M=1, qo=at, ko=at + (H + Hkv) * width, vo=at + H * width), EINVAL)])
+    # an output between an input's rows touches none of them
+    assert call(q=None, qo=None, k=None, ko=None, v=_rows(at, 1 << 16, 1 << 15, Dh), vo=at + Hkv * width, M=1, B=1) == EHIP
+    wide = _rows(at, 1 << 14, 1 << 13, Dh)
+    assert call(q=None, qo=None, k=None, ko=None, v=wide, vo=at + Hkv * width) == EHIP
+    assert call(q=None, qo=None, k=None, ko=None, v=wide, vo=at + Hkv * width - 16) == EINVAL
