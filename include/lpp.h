@@ -422,7 +422,7 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  * does not see plays no part in it, whatever it holds.  Scores (scale times the product) are to stay below 10^29 in
  * magnitude.  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments
  * give the same bits; sums are added in an order that depends on B and S, and in batches of 2 to 64 items on all lengths.
- * Errors: LPP_EINVAL (null, out an input, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
+ * Errors: LPP_EINVAL (null, out or the workspace over an input or over each other, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
  * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, 2^31 blocks), LPP_ENOWORKSPACE,
  * LPP_EHIP.
  */

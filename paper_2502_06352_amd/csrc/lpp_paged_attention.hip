@@ -33,6 +33,7 @@
 
 #include "lpp_device.h"
 #include "lpp_internal.h"
+#include "lpp_overlap.h"
 #include "lpp_paged_plan.h"
 #include "lpp_reciprocal.h"
 
@@ -954,7 +955,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
                         const int32_t* seq_len, const int32_t* row_len, int32_t B, int32_t H, int32_t M, int32_t S, float scale,
                         void* out, void* ws, size_t ws_bytes, void* stream) {
   if (!cache || !q || !k_new || !v_new || !out) return LPP_EINVAL;
-  if (out == q || out == k_new || out == v_new) return LPP_EINVAL;       // blocks read what others have finished
+  if (out == q || out == k_new || out == v_new || out == k_pages || out == v_pages) return LPP_EINVAL;      // (and see below)
   if (B < 1 || H < 1 || M < 1 || S < 0) return LPP_EINVAL;
   if (S > 0 && (!k_pages || !v_pages || !page_table || table_stride < 1)) return LPP_EINVAL;
   if (H % cache->Hkv != 0) return LPP_EINVAL;
@@ -971,6 +972,16 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   if (p.o_bytes > 0 && (!ws || misaligned(ws) || ws_bytes < paged_room(cache, B, gq, M, S))) return LPP_ENOWORKSPACE;
   if (!cache->d_counters || (tree && !tree->d_anc)) return LPP_EHIP;     // host-only handle: no device
   if (!lpp_is_current(cache->device) || (tree && tree->device != cache->device)) return LPP_EINVAL;
+  // blocks read what others have finished, and parts that others have left: neither lies in an input or in the other
+  const uint64_t row_bytes = (uint64_t)cache->Dh * esz, n_q = (uint64_t)B * H * M * row_bytes, n_new = (uint64_t)B * cache->Hkv * M * row_bytes;
+  const uint64_t n_pool = S > 0 ? ((uint64_t)cache->n_pages * cache->Hkv << cache->page_shift) * row_bytes : 0;
+  const uint64_t n_table = S > 0 ? (uint64_t)B * table_stride * 4 : 0, n_lens = (uint64_t)B * 4, n_parts = p.o_bytes + p.ml_bytes;
+  const auto meets_input = [&](const void* x, uint64_t n) {
+    return ranges_meet(x, n, q, n_q) || ranges_meet(x, n, k_new, n_new) || ranges_meet(x, n, v_new, n_new) || ranges_meet(x, n, k_pages, n_pool) ||
+           ranges_meet(x, n, v_pages, n_pool) || ranges_meet(x, n, page_table, n_table) || ranges_meet(x, n, seq_len, n_lens) ||
+           ranges_meet(x, n, row_len, n_lens);
+  };
+  if (meets_input(out, n_q) || meets_input(ws, n_parts) || ranges_meet(out, n_q, ws, n_parts)) return LPP_EINVAL;
   if (scale == 0.f) scale = 1.0f / sqrtf((float)cache->Dh);
   PagedAttnArgs a;
   a.q = q; a.kp = k_pages; a.vp = v_pages; a.kn = k_new; a.vn = v_new; a.out = out;

@@ -104,6 +104,35 @@ def test_one_workspace_for_calls_of_all_sizes(dtype, H, Hkv, Dh, largest, calls)
         assert bool((whole[n:] == 165).all())
 
 
+def test_outputs_and_workspaces_over_inputs_are_refused():
+    """Tensors that are parts of one buffer: what lies in an input, or out and the workspace in each other, is not enqueued."""
+    c = Case(1, 8, 2, 128, 16, [3000], parent=TINY, seed=80)
+    t = c.upload()
+    want, n = c.call(t).clone(), t["out"].numel()
+
+    def status(**kw):
+        with pytest.raises(lpp.LppError) as e:
+            c.call(dict(t, **kw))
+        return e.value.status
+
+    one = torch.zeros(2 * n, dtype=torch.bfloat16, device=DEV)
+    one[:n] = t["q"].view(-1)
+    q = one[:n].view(t["q"].shape)
+    for at in (0, 8, n - 8):
+        assert status(q=q, out=one[at:at + n].view(q.shape)) == lpp.LPP_EINVAL
+    for name in ("kp", "vp"):
+        assert status(out=t[name].view(-1)[64:64 + n].view(q.shape)) == lpp.LPP_EINVAL
+    parts, pool = t["ws"].numel(), t["kp"].view(-1).view(torch.uint8)
+    long = torch.cat([pool, torch.zeros(parts, dtype=torch.uint8, device=DEV)])
+    kp = long[:pool.numel()].view(torch.bfloat16).view(t["kp"].shape)
+    assert status(kp=kp, ws=long[256:256 + parts]) == lpp.LPP_EINVAL
+    both = torch.zeros(parts + 2 * n, dtype=torch.uint8, device=DEV)
+    assert status(ws=both[:parts], out=both[:2 * n].view(torch.bfloat16).view(q.shape)) == lpp.LPP_EINVAL
+    out = both[parts:].view(torch.bfloat16).view(q.shape)
+    assert torch.equal(c.call(dict(t, q=q, ws=both[:parts], out=out)), want)          # side by side
+    assert torch.equal(c.call(dict(t, q=q, out=one[n:].view(q.shape))), want)
+
+
 def test_rotary_outputs_over_inputs_are_refused():
     tree, rotary = lpp.Tree(TINY), lpp.Rotary(64)
     B, M, H, Hkv, Dh = 2, 16, 4, 2, 64

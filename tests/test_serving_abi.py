@@ -283,3 +283,11 @@ def test_rotary_refuses_outputs_over_inputs_and_each_other(L):
     wide = _rows(at, 1 << 14, 1 << 13, Dh)
     assert call(q=None, qo=None, k=None, ko=None, v=wide, vo=at + Hkv * width) == EHIP
     assert call(q=None, qo=None, k=None, ko=None, v=wide, vo=at + Hkv * width - 16) == EINVAL
+
+
+@no_gpu
+def test_attention_over_its_pages_is_refused(L):
+    cache, tree = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0])
+    for kp, vp, status in ((3 * FAKE, 4 * FAKE, EHIP), (2 * FAKE, 4 * FAKE, EINVAL), (3 * FAKE, 2 * FAKE, EINVAL)):
+        assert L.lpp_paged_tree_attention(cache.handle, tree.handle, FAKE, kp, vp, FAKE, 3, FAKE, FAKE, None, 2, 4, 40, 0.0, 2 * FAKE, FAKE,
+                                          1 << 20, None) == status
