@@ -414,13 +414,13 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  *   S         [host] no item has more cached positions (seq_len is clamped to it); decides how the launch is cut, so that a bound far
  *             above the lengths costs time.  S = 0: nothing is cached, pages and table may be NULL.  table_stride * page_size >= S
  *   seq_len   [device] int32 [B] or NULL (= S);  row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M)
- *   scale     0 selects 1/sqrt(Dh); negative, infinite or NaN is LPP_EINVAL
+ *   scale     0 selects 1/sqrt(Dh); negative, NaN, infinite or above 2 * 10^38 is LPP_EINVAL
  *   ws        lpp_paged_attention_workspace(cache, B, H, M, S) bytes, a number that grows with all four: a workspace made for the
  *             largest sizes serves every call of no more items, heads, rows and positions on a handle of the same geometry.  At most 768 rows of
  *             Dh + 2 floats a compute unit (102 MB for Dh 128)
  * Softmax and accumulation are float32; bf16 products run on the bf16 matrix cores with the weights rounded to bf16.  What a row
- * does not see plays no part in it, whatever it holds.  Scores (scale times the product) are to stay below 10^29 in
- * magnitude.  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments
+ * does not see plays no part in it, whatever it holds.  Scores (scale times the product) are to stay below 10^9 in
+ * magnitude (float32: 10^29).  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments
  * give the same bits; sums are added in an order that depends on B and S, and in batches of 2 to 64 items on all lengths.
  * Errors: LPP_EINVAL (null, out or the workspace over an input or over each other, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
  * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, 2^31 blocks), LPP_ENOWORKSPACE,

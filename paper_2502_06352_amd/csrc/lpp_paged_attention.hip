@@ -12,6 +12,8 @@
 // K and V go from memory to LDS without passing registers; the next tile's are on their way while one is worked on.  16-byte
 // pieces of a row lie in LDS in an order that depends on the row (swizzle), so that neither product's reads meet on a bank; the
 // order is made by where each lane reads from, as a wave's 64 pieces always land one behind the other.
+// A weight is 2^(s scale - reference) by one fused operation, and the reference the rounded product of the largest s: half of its last
+// place is in all of a row's exponents, 64 at scores of 10^9, which numbers and sums can take.
 // Sums, maxima and accumulators are float32.  P is rounded to bf16 for the second product, as its inputs are; a row's sum is
 // taken of the rounded weights.
 //
@@ -43,6 +45,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kMasked = -1.0e30f;  // finite stand-in for -inf
 constexpr float kLazy = 8.0f;        // log2 of the largest weight before a rescale
+constexpr float kLog2e = 1.44269504088896340736f;
 
 struct PagedAttnArgs {
   const void* q; const void* kp; const void* vp; const void* kn; const void* vn;
@@ -508,10 +511,10 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (bits >> (8 * (r >> 2) + (r & 3))) & 1u ? s[r] : -INFINITY;
     }
-    float mx = kMasked;
+    float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = mx > 0.5f * kMasked ? mx * a.scale : kMasked;               // (scale > 0: the maximum commutes with it)
+    mx = fmaxf(mx * a.scale, kMasked);               // (scale > 0: the maximum commutes with it; the product alone may lie far below)
     if (__ballot(mx > m_ref + kLazy)) {              // some row's reference moves: rare behind the first tile
       const float v = fmaxf(mx, __shfl_xor(mx, 32));
       const float nm = v > m_ref + kLazy ? v : m_ref;
@@ -960,7 +963,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   if (S > 0 && (!k_pages || !v_pages || !page_table || table_stride < 1)) return LPP_EINVAL;
   if (H % cache->Hkv != 0) return LPP_EINVAL;
   if (S > 0 && ((int64_t)table_stride << cache->page_shift) < S) return LPP_EINVAL;
-  if (!(scale >= 0.f) || scale == INFINITY) return LPP_EINVAL;           // NaN, negative, infinite
+  if (!(scale >= 0.f && scale <= 2e38f)) return LPP_EINVAL;                 // NaN, negative, infinite in base two
   if (misaligned(q) || misaligned(k_new) || misaligned(v_new) || misaligned(out) || misaligned(k_pages) || misaligned(v_pages)) return LPP_EINVAL;
   const int esz = cache->dtype == LPP_F32 ? 4 : 2, gq = H / cache->Hkv;
   // 32-bit offsets inside one head's new rows, row and key numbers, units and blocks
@@ -993,7 +996,7 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   a.row_blocks = p.row_blocks; a.nsplit = p.nsplit; a.range = p.range;
   a.share = (seq_len || row_len) && looks_at_lengths(cache, B, p) ? B : 0;
   a.units = (uint32_t)units; a.whole = (uint32_t)(units & ~7ll);
-  a.scale = cache->dtype == LPP_F32 ? scale : scale * 1.44269504088896340736f;
+  a.scale = cache->dtype == LPP_F32 ? scale : scale * kLog2e;
   a.ws_o = reinterpret_cast<float*>(ws);
   a.ws_ml = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(ws) + p.o_bytes);
   a.ws_o_bytes = (uint32_t)p.o_bytes; a.ws_ml_bytes = (uint32_t)p.ml_bytes;

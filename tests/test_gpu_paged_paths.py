@@ -146,3 +146,21 @@ def test_rotary_outputs_over_inputs_are_refused():
         assert e.value.status == lpp.LPP_EINVAL
     torch.cuda.synchronize()
     assert all(bool((o == 7.0).all()) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("parent,rows,sign,big,scale", [(TINY, None, 1, 15, 0.5), (XXL, None, -1, 15, 0.5), (None, [140, 77], 1, 15, 0.5),
+                                                       (TINY, None, -1, 50, 2.0 ** -71), (XXL, None, -1, 50, 2.0 ** -71),
+                                                       (None, [140, 77], -1, 50, 2.0 ** -71), (XXL, None, 1, -40, 2.0 ** 109)])
+def test_scores_of_nearly_ten_to_the_ninth(parent, rows, sign, big, scale, dtype):
+    """One number of a head makes the score, so that products are exact and scores differ by millions or not at all: a row's
+    result is the mean of the values whose score is the largest that it sees."""
+    c = Case(2, 4, 2, 64, 16, [400, 130], M=140, parent=parent, rows=rows, dtype=dtype, seed=81)
+    rng = np.random.default_rng(82)
+    for x in (c.kp, c.kn):
+        x[..., 1:][~np.isnan(x[..., 1:])] = 0.0
+        steps = 1.0 + rng.integers(0, 100, x[..., 0].shape) / 128.0
+        x[..., 0] = np.where(np.isnan(x[..., 0]), np.nan, sign * steps * 2.0 ** big)
+    c.q[..., 1:], c.q[..., 0] = 0.0, 2.0 ** big
+    t = c.upload()
+    c.check(c.call(t, scale=scale), scale=scale)

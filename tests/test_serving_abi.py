@@ -291,3 +291,11 @@ def test_attention_over_its_pages_is_refused(L):
     for kp, vp, status in ((3 * FAKE, 4 * FAKE, EHIP), (2 * FAKE, 4 * FAKE, EINVAL), (3 * FAKE, 2 * FAKE, EINVAL)):
         assert L.lpp_paged_tree_attention(cache.handle, tree.handle, FAKE, kp, vp, FAKE, 3, FAKE, FAKE, None, 2, 4, 40, 0.0, 2 * FAKE, FAKE,
                                           1 << 20, None) == status
+
+
+@no_gpu
+def test_a_scale_that_overflows_in_base_two_is_refused(L):
+    cache, tree = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0])
+    for scale, status in ((3e38, EINVAL), (2.01e38, EINVAL), (2e38, EHIP), (1e-45, EHIP)):
+        assert L.lpp_paged_tree_attention(cache.handle, tree.handle, FAKE, 3 * FAKE, 3 * FAKE, FAKE, 3, FAKE, FAKE, None, 2, 4, 40, scale, 2 * FAKE,
+                                          FAKE, 1 << 20, None) == status
