@@ -20,12 +20,13 @@ inline bool rows_meet(const void* data, int64_t item, int64_t row, int64_t head,
   const int64_t first = (int64_t)(uintptr_t)data, lo = (int64_t)(uintptr_t)out, hi = lo + n;
   const int64_t end = first + (B - 1) * item + (M - 1) * row + (heads - 1) * head + width;
   if (first >= hi || end <= lo) return false;
-  if (head == 0) heads = 1;
+  if (item == M * row) { M *= B; B = 1; }
+  if (row == 0) M = 1;
   for (int64_t b = 0; b < (item == 0 ? 1 : B); ++b)
-    for (int64_t i = 0; i < (row == 0 ? 1 : M); ++i) {
-      const int64_t at = first + b * item + i * row;                 // the first head's row; head h's begins at at + h head
-      const int64_t h = lo - width < at || head == 0 ? 0 : (lo - width - at) / head + 1;      // the first that ends behind lo
-      if (h < heads && at + h * head < hi && at + h * head + width > lo) return true;
+    for (int64_t h = 0; h < (head == 0 ? 1 : heads); ++h) {
+      const int64_t at = first + b * item + h * head;                // row i begins at at + i row
+      const int64_t i = lo - width < at || row == 0 ? 0 : (lo - width - at) / row + 1;        // the first that ends behind lo
+      if (i < M && at + i * row < hi && at + i * row + width > lo) return true;
     }
   return false;
 }
