@@ -391,8 +391,8 @@ int32_t lpp_paged_destroy(lpp_paged* cache);
  * at or past it are dropped, lengths are clamped to it.  new_len may be NULL and must not be one of the inputs.
  * lpp_paged_append_kv: rows 0 .. row_len[b] - 1 of k_new / v_new [device] [B, Hkv, M, Dh] instead (a chunk of a prompt);
  * row_len [device] int32 [B] (clamped to [0, M]) or NULL (= M for every item).
- * Errors: LPP_EINVAL (null, sizes < 1, new_len an input, tensors not 16-byte aligned), LPP_EUNSUPPORTED (capacity + M or the
- * launch's blocks beyond 2^31), LPP_EHIP.
+ * Errors: LPP_EINVAL (null, sizes < 1, new_len an input, tensors not 16-byte aligned), LPP_EUNSUPPORTED (capacity + M beyond 2^31,
+ * a launch of 2^32 lanes: 256 for every kept row, or every 4 KiB of a head's new rows), LPP_EHIP.
  */
 int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* tree, const void* k_tree, const void* v_tree,
                             const int32_t* path, const int32_t* accept_len, const int32_t* page_table,
@@ -423,7 +423,7 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  * magnitude (float32: 10^29).  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments
  * give the same bits; sums are added in an order that depends on B and S, and in batches of 2 to 64 items on all lengths.
  * Errors: LPP_EINVAL (null, out or the workspace over an input or over each other, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
- * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, 2^31 blocks), LPP_ENOWORKSPACE,
+ * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, a launch of 2^32 lanes: at most 512 for 16 rows of a key/value head, less for more), LPP_ENOWORKSPACE,
  * LPP_EHIP.
  */
 size_t  lpp_paged_attention_workspace(const lpp_paged* cache, int32_t B, int32_t H, int32_t M, int32_t S);
@@ -459,7 +459,7 @@ int32_t lpp_paged_chunk_attention(const lpp_paged* cache, const void* q, const v
  *                       if the strides are the output's, and must overlap no input otherwise, nor another output
  * The handle lives on the host (it may be used on any device).  Errors: LPP_EINVAL (null, sizes < 1, tree of another M, dim > Dh,
  * an unknown enumerator, a config out of range, misaligned, outputs that overlap what they must not), LPP_EUNSUPPORTED (dtype, dim or Dh not a multiple of
- * 16 or too large, strides not multiples of 16 bytes), LPP_EHIP.
+ * 16 or too large, strides not multiples of 16 bytes, a launch of 2^32 lanes: 256 for every two heads of up to 4096 / Dh rows), LPP_EHIP.
  */
 #define LPP_ROTARY_MAX_DIM     256
 #define LPP_ROTARY_HALF        0
@@ -512,7 +512,8 @@ int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree, int32_t d
  * lpp_commit_counts   adds what a step emitted: the tokens of the accepted path and final_token, as lpp_relaxed_verify wrote
  *                     them (an item whose walk gave up adds nothing).
  * Errors: LPP_EINVAL (null, sizes < 1, vocab_offset < 0, vocab_offset + V > ldv, cfg_scale NaN, negative strides, bf16 in place),
- * LPP_EUNSUPPORTED (dtype unknown, launch beyond 2^31 blocks), LPP_EHIP.
+ * LPP_EUNSUPPORTED (dtype unknown, a launch of 2^32 lanes: 256 for every row and 2048 tokens of it; counts: 1024 for every item and 32768
+ * tokens, 64 for an item's step), LPP_EHIP.
  */
 typedef struct lpp_logits_options {
   const void*     uncond_logits;

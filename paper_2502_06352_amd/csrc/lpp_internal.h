@@ -69,6 +69,9 @@ inline bool lpp_is_current(int device) {
   return now == device;
 }
 
+// Whether a launch can have so many blocks: their lanes are numbered in 32 bits.
+inline bool lpp_launch_fits(int64_t blocks, int threads) { return blocks < (1ll << 32) / threads; }
+
 // The largest dynamic LDS size a kernel has been enabled for so far, per device: the attribute
 // (hipFuncAttributeMaxDynamicSharedMemorySize) belongs to one device's copy of the kernel.  One
 // such cache per kernel, zero-initialised; `floor` is what a kernel may use without asking.

@@ -182,7 +182,6 @@ int32_t launch_adjust(LogitsArgs& a, int64_t rows, int32_t n_cu, hipStream_t s) 
   const bool two = rows * wide >= (int64_t)n_cu * 4;
   a.parts = (int32_t)(two ? wide : narrow);
   const int64_t blocks = rows * a.parts;
-  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
   if (two) hipLaunchKernelGGL((adjust_logits_kernel<T, GUIDED, 2>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((adjust_logits_kernel<T, GUIDED, 1>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   LPP_HIP_TRY(hipGetLastError());
@@ -211,7 +210,7 @@ extern "C" int32_t lpp_adjust_logits(const lpp_tree* tree, int32_t dtype, const 
   a.mask = opts->mask; a.mask_item = opts->mask_item_stride; a.mask_row = opts->mask_row_stride;
   a.ldv = ldv; a.V = V; a.M = tree->M; a.words = tree->words; a.cfg_scale = opts->cfg_scale;
   const int64_t rows = (int64_t)B * tree->M;
-  if (rows * (((int64_t)V + 2047) / 2048) > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  if (!lpp_launch_fits(rows * (((int64_t)V + 2047) / 2048), 256)) return LPP_EUNSUPPORTED;     // (narrower blocks: few)
   if (!tree->d_anc) return LPP_EHIP;                         // host-only handle: no device
   if (!lpp_is_current(tree->device)) return LPP_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -223,7 +222,7 @@ extern "C" int32_t lpp_token_counts(const int32_t* tokens, const int32_t* len, i
                                     void* stream) {
   if (!counts || B < 1 || T < 0 || V < 1 || (T > 0 && !tokens)) return LPP_EINVAL;
   const int64_t pieces = ((int64_t)V + kCounted - 1) / kCounted, blocks = B * pieces;
-  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  if (!lpp_launch_fits(blocks, 1024)) return LPP_EUNSUPPORTED;
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) {
     (void)hipGetLastError();
@@ -243,6 +242,7 @@ extern "C" int32_t lpp_commit_counts(const lpp_tree* tree, const int32_t* tokens
                                      const int32_t* final_token, int32_t B, int32_t V, int32_t* counts, void* stream) {
   if (!tree || !tokens || !path || !accept_len || !final_token || !counts) return LPP_EINVAL;
   if (B < 1 || V < 1) return LPP_EINVAL;
+  if (!lpp_launch_fits(B, 64)) return LPP_EUNSUPPORTED;
   if (!tree->d_anc) return LPP_EHIP;
   if (!lpp_is_current(tree->device)) return LPP_EINVAL;
   hipLaunchKernelGGL(commit_counts_kernel, dim3((unsigned)B), dim3(64), 0, reinterpret_cast<hipStream_t>(stream), tokens, path,

@@ -155,7 +155,7 @@ extern "C" int32_t lpp_paged_commit_kv(const lpp_paged* cache, const lpp_tree* t
   a.path = tree->depth > 0 ? path : seq_len; a.accept_len = accept_len;
   a.depth = tree->depth > 0 ? tree->depth : 1;
   const int64_t blocks = (int64_t)B * (a.depth + 1);
-  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  if (!lpp_launch_fits(blocks, 256)) return LPP_EUNSUPPORTED;
   if (!cache->d_counters || !tree->d_anc) return LPP_EHIP;   // host-only handle: no device
   if (!lpp_is_current(cache->device)) return LPP_EINVAL;
   hipLaunchKernelGGL(paged_commit_kernel, dim3((unsigned)blocks), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
@@ -173,7 +173,7 @@ extern "C" int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new
   a.row_len = row_len;
   a.tiles = (int32_t)((((int64_t)M << a.chunk_shift) + 255) >> 8);
   const int64_t blocks = (int64_t)B * cache->Hkv * a.tiles;
-  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  if (!lpp_launch_fits(blocks, 256)) return LPP_EUNSUPPORTED;
   if (!cache->d_counters) return LPP_EHIP;
   if (!lpp_is_current(cache->device)) return LPP_EINVAL;
   hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)blocks), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);

@@ -971,7 +971,8 @@ int32_t paged_attention(const lpp_paged* cache, const lpp_tree* tree, const void
   if ((int64_t)B * cache->Hkv >= (1ll << 24)) return LPP_EUNSUPPORTED;
   const PagedPlan p = plan_paged(cache, B, gq, M, S);
   const int64_t units = (int64_t)B * cache->Hkv * p.nsplit;
-  if (units * p.row_blocks >= (1ll << 31)) return LPP_EUNSUPPORTED;
+  const int waves = cache->dtype == LPP_BF16 ? p.rows / 32 * p.wk : p.wk;
+  if (!lpp_launch_fits(units * p.row_blocks, waves * 64)) return LPP_EUNSUPPORTED;
   if (p.o_bytes > 0 && (!ws || misaligned(ws) || ws_bytes < paged_room(cache, B, gq, M, S))) return LPP_ENOWORKSPACE;
   if (!cache->d_counters || (tree && !tree->d_anc)) return LPP_EHIP;     // host-only handle: no device
   if (!lpp_is_current(cache->device) || (tree && tree->device != cache->device)) return LPP_EINVAL;

@@ -221,14 +221,6 @@ extern "C" int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree
   }
   if (tree && !tree->d_anc) return LPP_EHIP;                 // host-only handle: no device
   if (tree && !lpp_is_current(tree->device)) return LPP_EINVAL;
-  // blocks read what others have written: outputs lie in no input (but in place, see above) and in no other output
-  for (int t = 0; t < 3; ++t)
-    for (int u = 0; u < 3 && out[t]; ++u) {
-      const int64_t width = (int64_t)Dh * esz, n = (int64_t)B * a.n_heads[t] * M * width;
-      if (in[u] && !(u == t && in[u]->data == out[t]) &&
-          rows_meet(in[u]->data, in[u]->item * esz, in[u]->row * esz, in[u]->head * esz, B, M, a.n_heads[u], width, out[t], n)) return LPP_EINVAL;
-      if (u > t && ranges_meet(out[t], (uint64_t)n, out[u], (uint64_t)B * a.n_heads[u] * M * width)) return LPP_EINVAL;
-    }
   a.first_pos = first_pos; a.row_len = row_len;
   a.anc = tree ? tree->d_anc : nullptr; a.words = tree ? tree->words : 0;
   a.M = M; a.Dh = Dh; a.dim = rotary->dim; a.magnitude = rotary->magnitude;
@@ -239,7 +231,15 @@ extern "C" int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree
   a.groups = (a.heads + a.group - 1) / a.group;
   std::copy(rotary->turns, rotary->turns + LPP_ROTARY_MAX_DIM / 2, a.turns);
   const int64_t blocks = (int64_t)B * a.row_blocks * a.groups;
-  if (blocks > 0x7FFFFFFF) return LPP_EUNSUPPORTED;
+  if (!lpp_launch_fits(blocks, 256)) return LPP_EUNSUPPORTED;
+  // blocks read what others have written: outputs lie in no input (but in place, see above) and in no other output
+  for (int t = 0; t < 3; ++t)
+    for (int u = 0; u < 3 && out[t]; ++u) {
+      const int64_t width = (int64_t)Dh * esz, n = (int64_t)B * a.n_heads[t] * M * width;
+      if (in[u] && !(u == t && in[u]->data == out[t]) &&
+          rows_meet(in[u]->data, in[u]->item * esz, in[u]->row * esz, in[u]->head * esz, B, M, a.n_heads[u], width, out[t], n)) return LPP_EINVAL;
+      if (u > t && ranges_meet(out[t], (uint64_t)n, out[u], (uint64_t)B * a.n_heads[u] * M * width)) return LPP_EINVAL;
+    }
   const dim3 grid((unsigned)blocks);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool half = rotary->layout == LPP_ROTARY_HALF;

@@ -299,3 +299,42 @@ def test_a_scale_that_overflows_in_base_two_is_refused(L):
     for scale, status in ((3e38, EINVAL), (2.01e38, EINVAL), (2e38, EHIP), (1e-45, EHIP)):
         assert L.lpp_paged_tree_attention(cache.handle, tree.handle, FAKE, 3 * FAKE, 3 * FAKE, FAKE, 3, FAKE, FAKE, None, 2, 4, 40, scale, 2 * FAKE,
                                           FAKE, 1 << 20, None) == status
+
+
+@no_gpu
+def test_launches_of_more_lanes_than_can_be_numbered_are_refused(L):
+    """2^32 lanes and more, and the largest number of items below."""
+    cache, tree, rotary = lpp.PagedCache(lpp.LPP_BF16, 2, 64, 16, 4), lpp.Tree([-1, 0, 0]), lpp.Rotary(64)
+    far = [n << 44 for n in range(1, 7)]
+
+    def commit(B):                                                 # two kept rows an item
+        return L.lpp_paged_commit_kv(cache.handle, tree.handle, FAKE, FAKE, FAKE, FAKE, FAKE, 3, FAKE, B, FAKE, FAKE, None, None)
+
+    def append(B):                                                 # two heads of one block
+        return L.lpp_paged_append_kv(cache.handle, FAKE, FAKE, None, FAKE, 3, FAKE, B, 5, FAKE, FAKE, None, None)
+
+    def turn(B):                                                   # eight heads, two a block
+        return L.lpp_rotary_qkv(rotary.handle, None, lpp.LPP_BF16, _rows(far[0]), _rows(far[1]), _rows(far[2]), None, None, B, 4, 2, 5, 64, far[3],
+                                far[4], far[5], None)
+
+    opts = lpp.binding._pack_logits(*[0] * 12)
+
+    def logits(B):                                                 # three rows
+        return L.lpp_adjust_logits(tree.handle, lpp.LPP_F32, FAKE, 100, 4, 90, B, opts, FAKE, None)
+
+    def counts(B):
+        return L.lpp_token_counts(FAKE, None, B, 7, 90, FAKE, None)
+
+    def commit_counts(B):
+        return L.lpp_commit_counts(tree.handle, FAKE, FAKE, FAKE, FAKE, B, 90, FAKE, None)
+
+    for call, first in ((commit, 1 << 23), (append, 1 << 23), (turn, 1 << 22), (logits, (1 << 24) // 3 + 1), (counts, 1 << 22),
+                        (commit_counts, 1 << 26)):
+        assert call(first) == EUNSUP and call(0x7FFFFFFF) == EUNSUP, call
+        assert call(first - 1) == EHIP, call
+
+    def chunk(B):                                                  # two heads of 200 rows, blocks of at least 256 lanes
+        return L.lpp_paged_chunk_attention(cache.handle, FAKE, FAKE, FAKE, FAKE, 3, FAKE, FAKE, None, None, B, 4, 100, 40, 0.0, 2 * FAKE, FAKE, 1 << 30,
+                                           None)
+
+    assert chunk(1 << 22) == EUNSUP and chunk(1 << 18) == EHIP
