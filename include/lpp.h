@@ -459,7 +459,7 @@ int32_t lpp_paged_chunk_attention(const lpp_paged* cache, const void* q, const v
  *                       if the strides are the output's, and must overlap no input otherwise, nor another output
  * The handle lives on the host (it may be used on any device).  Errors: LPP_EINVAL (null, sizes < 1, tree of another M, dim > Dh,
  * an unknown enumerator, a config out of range, misaligned, outputs that overlap what they must not), LPP_EUNSUPPORTED (dtype, dim or Dh not a multiple of
- * 16 or too large, strides not multiples of 16 bytes, a launch of 2^32 lanes: 256 for every two heads of up to 4096 / Dh rows), LPP_EHIP.
+ * 16 or too large, strides not multiples of 16 bytes, M of 2^30 and more, a launch of 2^32 lanes: 256 for every two heads of up to 4096 / Dh rows), LPP_EHIP.
  */
 #define LPP_ROTARY_MAX_DIM     256
 #define LPP_ROTARY_HALF        0
@@ -512,7 +512,7 @@ int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree, int32_t d
  * lpp_commit_counts   adds what a step emitted: the tokens of the accepted path and final_token, as lpp_relaxed_verify wrote
  *                     them (an item whose walk gave up adds nothing).
  * Errors: LPP_EINVAL (null, sizes < 1, vocab_offset < 0, vocab_offset + V > ldv, cfg_scale NaN, negative strides, bf16 in place),
- * LPP_EUNSUPPORTED (dtype unknown, a launch of 2^32 lanes: 256 for every row and 2048 tokens of it; counts: 1024 for every item and 32768
+ * LPP_EUNSUPPORTED (dtype unknown, V or T of 2^30 and more, a launch of 2^32 lanes: 256 for every row and 2048 tokens of it; counts: 1024 for every item and 32768
  * tokens, 64 for an item's step), LPP_EHIP.
  */
 typedef struct lpp_logits_options {

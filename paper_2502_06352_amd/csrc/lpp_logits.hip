@@ -153,8 +153,8 @@ __global__ __launch_bounds__(1024) void token_counts_kernel(const int32_t* token
   __syncthreads();
   const int32_t* t = tokens + (int64_t)b * T;
   for (int j = threadIdx.x; j < n; j += 1024) {
-    const int x = t[j] - x0;
-    if (t[j] >= 0 && x >= 0 && x < here) atomicAdd(&s_n[x], 1);
+    const int x = t[j];
+    if (x >= x0 && x - x0 < here) atomicAdd(&s_n[x - x0], 1);
   }
   __syncthreads();
   int32_t* out = counts + (int64_t)b * V + x0;
@@ -197,6 +197,7 @@ extern "C" int32_t lpp_adjust_logits(const lpp_tree* tree, int32_t dtype, const 
   if (opts->cfg_scale != opts->cfg_scale) return LPP_EINVAL;
   if (opts->bias_stride < 0 || opts->mask_item_stride < 0 || opts->mask_row_stride < 0) return LPP_EINVAL;
   if (dtype != LPP_F32 && dtype != LPP_BF16) return LPP_EUNSUPPORTED;
+  if (V >= 1 << 30) return LPP_EUNSUPPORTED;                 // (a lane's tokens are numbered past V)
   // what is written must not be read by another lane: in place with float32 logits only
   if (dtype != LPP_F32 && (out == logits || out == opts->uncond_logits)) return LPP_EINVAL;
   LogitsArgs a;
@@ -221,6 +222,7 @@ extern "C" int32_t lpp_adjust_logits(const lpp_tree* tree, int32_t dtype, const 
 extern "C" int32_t lpp_token_counts(const int32_t* tokens, const int32_t* len, int32_t B, int32_t T, int32_t V, int32_t* counts,
                                     void* stream) {
   if (!counts || B < 1 || T < 0 || V < 1 || (T > 0 && !tokens)) return LPP_EINVAL;
+  if (T >= 1 << 30 || V >= 1 << 30) return LPP_EUNSUPPORTED; // (lanes step past the last token)
   const int64_t pieces = ((int64_t)V + kCounted - 1) / kCounted, blocks = B * pieces;
   if (!lpp_launch_fits(blocks, 1024)) return LPP_EUNSUPPORTED;
   int ndev = 0;

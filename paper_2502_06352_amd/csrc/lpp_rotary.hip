@@ -194,6 +194,7 @@ extern "C" int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree
   if (rotary->dim > Dh) return LPP_EINVAL;
   if (dtype != LPP_F32 && dtype != LPP_BF16) return LPP_EUNSUPPORTED;
   if (Dh % 16 != 0 || Dh > LPP_ROTARY_MAX_DIM) return LPP_EUNSUPPORTED;
+  if (M >= 1 << 30) return LPP_EUNSUPPORTED;                 // (a block's rows are numbered past M)
   const int esz = dtype == LPP_F32 ? 4 : 2;
   const lpp_rows* in[3] = {q, k, v};
   void* out[3] = {q_out, k_out, v_out};

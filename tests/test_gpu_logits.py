@@ -149,3 +149,11 @@ def test_many_rows(kw):
     they are four a compute unit (here 1548 blocks)."""
     assert 4 * 129 * 3 >= 4 * torch.cuda.get_device_properties(0).multi_processor_count
     _run(WIDE, 4, 4097, 5, 3, seed=7, **kw)
+
+
+def test_tokens_far_outside_count_nowhere():
+    tokens = np.array([[-2 ** 31, 2 ** 31 - 1, 39999, 32768, -1, 40000, 32767, -2 ** 31 + 5, 39999]], dtype=np.int32)
+    out = torch.full((1, 40000), -9, dtype=torch.int32, device=DEV)
+    lpp.lpp_token_counts(dev(tokens), None, 1, 40000, out)
+    got = out.cpu().numpy()[0]
+    assert got.sum() == 4 and got[39999] == 2 and got[32768] == 1 and got[32767] == 1

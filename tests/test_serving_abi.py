@@ -338,3 +338,15 @@ def test_launches_of_more_lanes_than_can_be_numbered_are_refused(L):
                                            None)
 
     assert chunk(1 << 22) == EUNSUP and chunk(1 << 18) == EHIP
+
+
+@no_gpu
+def test_sizes_whose_numbers_would_not_fit_are_refused(L):
+    tree, rotary, far = lpp.Tree([-1, 0, 0]), lpp.Rotary(16), [n << 44 for n in range(1, 7)]
+    opts = lpp.binding._pack_logits(*[0] * 12)
+    for n, status in (((1 << 30) - 1, EHIP), (1 << 30, EUNSUP), (0x7FFFFFFF, EUNSUP)):
+        row = _rows(far[0], 0, 16, 0)
+        assert L.lpp_rotary_qkv(rotary.handle, None, lpp.LPP_BF16, row, None, None, None, None, 1, 2, 2, n, 16, far[3], None, None, None) == status
+        assert L.lpp_adjust_logits(tree.handle, lpp.LPP_F32, FAKE, 1 << 31, 0, n, 1, opts, FAKE, None) == status
+        assert L.lpp_token_counts(FAKE, None, 1, n, 90, FAKE, None) == status
+        assert L.lpp_token_counts(FAKE, None, 1, 7, n, FAKE, None) == status
