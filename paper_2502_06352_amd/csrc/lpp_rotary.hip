@@ -34,7 +34,8 @@ extern "C" int32_t lpp_rotary_create(const lpp_rotary_config* c, lpp_rotary** ou
   if (c->layout != LPP_ROTARY_HALF && c->layout != LPP_ROTARY_INTERLEAVED) return LPP_EINVAL;
   if (c->scaling < LPP_ROTARY_NONE || c->scaling > LPP_ROTARY_YARN) return LPP_EINVAL;
   const double base = c->base == 0. ? 10000. : c->base, fast = c->fast == 0. ? 32. : c->fast, slow = c->slow == 0. ? 1. : c->slow;
-  if (!(base > 1.) || !std::isfinite(base) || !(c->magnitude >= 0.) || !std::isfinite(c->magnitude)) return LPP_EINVAL;
+  if (!(base > 1.) || !std::isfinite(base) || !(c->magnitude >= 0.)) return LPP_EINVAL;
+  if (!std::isfinite((float)c->magnitude) || (c->magnitude > 0. && (float)c->magnitude == 0.f)) return LPP_EINVAL;      // (m is a float32)
   if (c->scaling != LPP_ROTARY_NONE && (!(c->factor >= 1.) || !std::isfinite(c->factor))) return LPP_EINVAL;
   if (c->scaling == LPP_ROTARY_YARN && (c->original_len < 1 || !(slow > 0.) || !(fast > slow) || !std::isfinite(fast))) return LPP_EINVAL;
   if (c->dim % 16 != 0 || c->dim > LPP_ROTARY_MAX_DIM) return LPP_EUNSUPPORTED;

@@ -350,3 +350,10 @@ def test_sizes_whose_numbers_would_not_fit_are_refused(L):
         assert L.lpp_adjust_logits(tree.handle, lpp.LPP_F32, FAKE, 1 << 31, 0, n, 1, opts, FAKE, None) == status
         assert L.lpp_token_counts(FAKE, None, 1, n, 90, FAKE, None) == status
         assert L.lpp_token_counts(FAKE, None, 1, 7, n, FAKE, None) == status
+
+
+def test_a_rotary_magnitude_is_a_float32(L):
+    for magnitude, status in ((1e39, EINVAL), (1e-60, EINVAL), (math.inf, EINVAL), (3e38, lpp.LPP_OK), (1e-30, lpp.LPP_OK)):
+        h = C.c_void_p()
+        assert L.lpp_rotary_create(C.byref(lpp.binding.RotaryConfig(dim=64, magnitude=magnitude)), C.byref(h)) == status
+        L.lpp_rotary_destroy(h)
