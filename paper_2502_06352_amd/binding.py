@@ -358,9 +358,9 @@ def _refuse(where: str, what: str):
 
 def _want(where: str, name: str, t, dtype, n: int, device: int) -> int:
     """Address of ``t``, which is to be ``n`` contiguous elements on ``device``."""
-    if t.dtype is _DTYPES.get(dtype) and t.numel() == n and t.is_contiguous() and t.get_device() == device:
+    if t is not None and t.dtype is _DTYPES.get(dtype) and t.numel() == n and t.is_contiguous() and t.get_device() == device:
         return t.data_ptr()
-    _refuse(where, f"{name} is of another type or size, has gaps, or is not on the current device")
+    _refuse(where, f"{name} is missing, of another type or size, has gaps, or is not on the current device")
 
 
 def _scratch(where: str, ws, device: int) -> Optional[int]:
@@ -394,17 +394,21 @@ class PagedCache:
 
 
 def _table(where: str, page_table, B: int, device: int) -> int:
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    if page_table is None or page_table.dim() != 2 or page_table.shape[0] != B:
         _refuse(where, "page_table is not [B, table_stride]")
     return _want(where, "page_table", page_table, "i32", page_table.numel(), device)
+
+
+def _path(where: str, tree: Tree, path, B: int) -> None:
+    if path is None or (tree.depth and path.numel() != B * tree.depth):
+        _refuse(where, "path is not [B, depth]")
 
 
 def lpp_paged_commit_kv(cache: PagedCache, tree: Tree, k_tree, v_tree, path, accept_len, page_table, seq_len, B: int,
                         k_pages, v_pages, new_len, stream=None) -> None:
     w, d, t = "lpp_paged_commit_kv", _device(), cache.dtype
     n = B * cache.Hkv * tree.M * cache.Dh
-    if tree.depth and path.numel() != B * tree.depth:
-        _refuse(w, "path is not [B, depth]")
+    _path(w, tree, path, B)
     _check(lib().lpp_paged_commit_kv(
         cache.handle, tree.handle, _want(w, "k_tree", k_tree, t, n, d), _want(w, "v_tree", v_tree, t, n, d),
         _want(w, "path", path, "i32", path.numel(), d) or _ptr(accept_len), _want(w, "accept_len", accept_len, "i32", B, d),
@@ -429,7 +433,7 @@ def lpp_paged_attention_workspace(cache: PagedCache, B: int, H: int, M: int, S: 
 
 
 def _pages(where: str, cache: PagedCache, k_pages, v_pages, page_table, B: int, S: int, device: int):
-    if S == 0 and page_table is None:
+    if S == 0:                                             # (nothing is cached: they are not read)
         return None, None, None, 0
     return (_want(where, "k_pages", k_pages, cache.dtype, cache.pool, device),
             _want(where, "v_pages", v_pages, cache.dtype, cache.pool, device), _table(where, page_table, B, device),
@@ -541,7 +545,7 @@ def lpp_adjust_logits(tree: Tree, dtype: int, logits, ldv: int, vocab_offset: in
 def lpp_token_counts(tokens, length, B: int, V: int, counts, stream=None) -> None:
     """``tokens``: [B, T];  ``length``: [B] or None (= T)."""
     w, d = "lpp_token_counts", _device()
-    if tokens.dim() != 2 or tokens.shape[0] != B:
+    if tokens is None or tokens.dim() != 2 or tokens.shape[0] != B:
         _refuse(w, "tokens is not [B, T]")
     _check(lib().lpp_token_counts(_want(w, "tokens", tokens, "i32", tokens.numel(), d), _maybe(w, "length", length, "i32", B, d),
                                   B, tokens.shape[1], V, _want(w, "counts", counts, "i32", B * V, d), _on(stream, d)), w)
@@ -549,8 +553,7 @@ def lpp_token_counts(tokens, length, B: int, V: int, counts, stream=None) -> Non
 
 def lpp_commit_counts(tree: Tree, tokens, path, accept_len, final_token, B: int, V: int, counts, stream=None) -> None:
     w, d = "lpp_commit_counts", _device()
-    if tree.depth and path.numel() != B * tree.depth:
-        _refuse(w, "path is not [B, depth]")
+    _path(w, tree, path, B)
     _check(lib().lpp_commit_counts(
         tree.handle, _want(w, "tokens", tokens, "i32", B * tree.M, d),
         _want(w, "path", path, "i32", path.numel(), d) or _ptr(accept_len), _want(w, "accept_len", accept_len, "i32", B, d),

@@ -357,3 +357,27 @@ def test_a_rotary_magnitude_is_a_float32(L):
         h = C.c_void_p()
         assert L.lpp_rotary_create(C.byref(lpp.binding.RotaryConfig(dim=64, magnitude=magnitude)), C.byref(h)) == status
         L.lpp_rotary_destroy(h)
+
+
+@no_gpu
+def test_the_binding_refuses_what_is_missing():
+    B, Hkv, M, Dh, n = 2, 2, 3, 64, 4
+    cache, tree = lpp.PagedCache(lpp.LPP_F32, Hkv, Dh, 16, n), lpp.Tree([-1, 0, 0])
+    new, pool, q = torch.zeros(B, Hkv, M, Dh), torch.zeros(n, Hkv, 16, Dh), torch.zeros(B, 4, M, Dh)
+    i32 = dict(dtype=torch.int32)
+    table, lens, path, tokens = torch.zeros(B, 2, **i32), torch.zeros(B, **i32), torch.zeros(B, tree.depth, **i32), torch.zeros(B, M, **i32)
+    x, counts, ws = torch.zeros(B, M, 40), torch.zeros(B, 40, **i32), torch.zeros(1 << 16, dtype=torch.uint8)
+    calls = [(lpp.lpp_paged_commit_kv, [cache, tree, new, new, path, lens, table, lens, B, pool, pool, None]),
+             (lpp.lpp_paged_append_kv, [cache, new, new, None, table, lens, B, M, pool, pool, None]),
+             (lpp.lpp_paged_tree_attention, [cache, tree, q, pool, pool, table, new, new, None, B, 4, 20, 0.0, q.clone(), ws]),
+             (lpp.lpp_paged_chunk_attention, [cache, q, pool, pool, table, new, new, None, None, B, 4, M, 20, 0.0, q.clone(), ws]),
+             (lpp.lpp_adjust_logits, [tree, lpp.LPP_F32, x, 40, 0, 40, B, x]), (lpp.lpp_token_counts, [tokens, None, B, 40, counts]),
+             (lpp.lpp_commit_counts, [tree, tokens, path, lens, lens, B, 40, counts])]
+    for call, args in calls:
+        assert _status(call, *args) == EHIP
+        for i, a in enumerate(args):
+            if torch.is_tensor(a) and a is not ws:
+                assert _status(call, *args[:i], None, *args[i + 1:]) == EINVAL, (call, i)
+    # nothing is cached: neither pages nor a table
+    for pages, t in ((None, None), (None, table), (pool, table)):
+        assert _status(lpp.lpp_paged_tree_attention, cache, tree, q, pages, pages, t, new, new, None, B, 4, 0, 0.0, q.clone(), ws) == EHIP
