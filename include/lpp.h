@@ -446,7 +446,8 @@ int32_t lpp_paged_chunk_attention(const lpp_paged* cache, const void* q, const v
  *   other numbers of a head, and the values, are copied.
  *   theta_j = base^(-2j / dim);  LPP_ROTARY_LINEAR: theta_j / factor;  LPP_ROTARY_NTK: base * factor^(dim / (dim - 2)) for
  *   base;  LPP_ROTARY_YARN: with r = original_len * theta_j / (2 pi) turns and g = clamp((r - slow) / (fast - slow), 0, 1),
- *   (1 - g) theta_j / factor + g theta_j, and m = 0.1 ln(factor) + 1.  m = 1 otherwise; `magnitude` > 0 sets m.
+ *   (1 - g) theta_j / factor + g theta_j, and m = 0.1 ln(factor) + 1 (the ramp is over turns; where it is taken over j between
+ *   rounded bounds the pairs between get other angles).  m = 1 otherwise; `magnitude` > 0 sets m.
  * Angles are formed in float64 and reduced before they are rounded: far positions are as exact as near ones.
  *   lpp_rotary_config   dim a multiple of 16 up to LPP_ROTARY_MAX_DIM; zeros select base 10000, fast 32, slow 1;
  *                       factor >= 1 (not read without scaling); original_len >= 1 (read by YARN only)
@@ -499,7 +500,8 @@ int32_t lpp_rotary_qkv(const lpp_rotary* rotary, const lpp_tree* tree, int32_t d
  *       is history)
  *   n > 0:  l = (l > 0 ? l / repetition[b] : l * repetition[b]) - frequency[b] n - presence[b]
  *   l = l + bias[x];   l = -inf where bit x % 32 of word x / 32 of the row's mask is 0, whatever l was
- * in float32; out[b, i, vocab_offset + x] = l.  Columns outside [vocab_offset, vocab_offset + V) are neither read nor
+ * in float32 (one count for all three penalties; where they go by different ones, a call with repetition, then one in place with the
+ * others); out[b, i, vocab_offset + x] = l.  Columns outside [vocab_offset, vocab_offset + V) are neither read nor
  * written.  A row whose mask allows nothing is -inf throughout: it has no distribution, and lpp_relaxed_verify wants one.
  *   logits, uncond_logits   [device] [B, M, ldv], float32 or bf16 (dtype);  out [device] float32 [B, M, ldv], which may be
  *                           either of the two where they are float32

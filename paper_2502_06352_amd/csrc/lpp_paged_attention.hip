@@ -24,11 +24,12 @@
 //
 // What bounds it (replayed; a copy moves 4.95 TB/s here, a large bf16 product reaches 1138 TFLOP/s): single tokens over long
 // caches the memory, 206 us and 5.5 TB/s for 16 items of 2048 to 32768 keys, 32 heads over 8 of 128.  Long chunks the matrix
-// cores' feed, 395 us and 980 TFLOP/s for 2 x 2048 rows over 8192 and 4096 keys (matrix cores busy 47 % of the cycles, vector
-// instructions 42 %, no bank conflicts).  Wide trees of heads of 64 the softmax, 62 us and 445 TFLOP/s for 16 trees of 129
-// rows, 24 heads over 8, up to 4096 keys (vector instructions 55 %, matrix cores 25 %; a tile's 16 exponentials a lane, their
-// products, maxima and sums take longer than its 8 matrix instructions), and there what a compute unit takes in, 53 bytes a ns
-// of the 58 seen at most.  Small calls the latency of one round: 10 us for a token over 2400 keys.
+// cores' feed, 394 us and 980 TFLOP/s for 2 x 2048 rows over 8192 and 4096 keys (matrix cores busy 47 % of the cycles, vector
+// instructions 42 %, no bank conflicts).  Wide trees of heads of 64 the softmax, 64 us and 430 TFLOP/s for 16 trees of 129
+// rows, 24 heads over 8, up to 4096 keys (vector instructions 54 %, matrix cores 25 %, one after the other in a wave: a tile's 16
+// exponentials a lane, their products, maxima and sums take longer than its 8 matrix instructions; the keys and values that come
+// in are 35 bytes a ns and compute unit of the 58 seen at most).  Small calls the latency of one round: 11 us for a token over 2400
+// keys.
 #include <math.h>
 
 #include <algorithm>
@@ -738,9 +739,10 @@ __global__ __launch_bounds__(WR * WK * 64) void paged_attn_bf16_kernel(PagedAttn
 
 // A block is NT tiles of 16 rows; its W waves take the 16-key tiles of its range in turn.  Lane (i, g) of a wave holds of key i
 // the dimensions 16 t + 4 g .. + 3, and of keys 4 g + r the values of dimensions 64 h + 4 i .. + 3: what its 16-byte loads
-// bring is what both products want.  Bound by what a compute unit takes in (every block reads all keys of its range: 41 bytes
-// a ns), or, where two tiles of rows share what is loaded, by the float32 matrix instructions (64 % of their rate, by count; 32
-// heads over 8 of 128, 1526 rows over 1380 keys: 602 us, 89 TFLOP/s of the 154 that a large product reaches).
+// bring is what both products want.  Single tokens over long caches are bound by memory (16 items of 2048 to 32768 keys, 32 heads
+// over 8 of 128: 413 us, 5.5 TB/s), small calls by latency (a token over 2400 keys: 15 us), rows enough for two tiles, which share what
+// is loaded, by matrix and vector instructions that follow each other and loads that are waited for at once (busy 60 % and 28 %
+// of the cycles with 32 heads over 8 of 128, 1526 rows over 1380 keys: 604 us, 89 TFLOP/s of the 154 that a large product reaches).
 template <int DH, int NT, int W>
 __global__ __launch_bounds__(W * 64) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int ROWS = 16 * NT, HT = DH / 64, P4 = DH / 4 + 1;

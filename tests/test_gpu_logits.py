@@ -157,3 +157,21 @@ def test_tokens_far_outside_count_nowhere():
     lpp.lpp_token_counts(dev(tokens), None, 1, 40000, out)
     got = out.cpu().numpy()[0]
     assert got.sum() == 4 and got[39999] == 2 and got[32768] == 1 and got[32767] == 1
+
+
+def test_penalties_that_go_by_different_counts():
+    """Repetition by prompt and output, then frequency and presence by the output alone: two calls, the second in place."""
+    rng = np.random.default_rng(8)
+    tree, B, V = lpp.Tree(SMALL), 2, 700
+    x = rng.standard_normal((B, tree.M, V), dtype=np.float32) * 3
+    tokens = rng.integers(0, 9, (B, tree.M)).astype(np.int32)
+    output = (rng.random((B, V)) < 0.2) * rng.integers(1, 5, (B, V))
+    both = output + (rng.random((B, V)) < 0.3)
+    rep, freq, pres = (np.array(v, dtype=np.float32) for v in ([1.3, 0.8], [0.25, 0.5], [-0.5, 1.0]))
+    out = torch.empty(B, tree.M, V, device=DEV)
+    lpp.lpp_adjust_logits(tree, lpp.LPP_F32, dev(x), V, 0, V, B, out, tokens=dev(tokens), counts=dev(both.astype(np.int32)), repetition=dev(rep))
+    lpp.lpp_adjust_logits(tree, lpp.LPP_F32, out, V, 0, V, B, out, tokens=dev(tokens), counts=dev(output.astype(np.int32)), frequency=dev(freq),
+                          presence=dev(pres))
+    first, size = adjust_logits(SMALL, x, tokens=tokens, counts=both, repetition=rep)
+    want, size = adjust_logits(SMALL, first, tokens=tokens, counts=output, frequency=freq, presence=pres)
+    assert np.all(np.abs(out.cpu().numpy() - want) <= 8 * 2.0 ** -24 * size)
