@@ -423,7 +423,7 @@ int32_t lpp_paged_append_kv(const lpp_paged* cache, const void* k_new, const voi
  * magnitude (float32: 10^29).  Results do not depend on what is in ws or in pages beyond the lengths, and two calls with the same arguments
  * give the same bits; sums are added in an order that depends on B and S, and in batches of 2 to 64 items on all lengths.
  * Errors: LPP_EINVAL (null, out or the workspace over an input or over each other, B/H/M < 1, S < 0, H % Hkv != 0, table too short, misaligned, tree and cache on different devices),
- * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, a launch of 2^32 lanes: at most 512 for 16 rows of a key/value head, less for more), LPP_ENOWORKSPACE,
+ * LPP_EUNSUPPORTED (M * Dh elements of 2 GiB and more, S + M or M * H / Hkv of 2^30 and more, B * Hkv of 2^24 and more, a launch of 2^32 lanes: up to 1024 for every 16 rows of a key/value head), LPP_ENOWORKSPACE,
  * LPP_EHIP.
  */
 size_t  lpp_paged_attention_workspace(const lpp_paged* cache, int32_t B, int32_t H, int32_t M, int32_t S);

@@ -164,3 +164,13 @@ def test_scores_of_nearly_ten_to_the_ninth(parent, rows, sign, big, scale, dtype
     c.q[..., 1:], c.q[..., 0] = 0.0, 2.0 ** big
     t = c.upload()
     c.check(c.call(t, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("dtype,kw", [
+    ("f32", dict(B=2, H=4, Hkv=2, Dh=128, page=32, lens=[900, 333], M=700, rows=[700, 413])),
+    ("f32", dict(B=3, H=3, Hkv=3, Dh=64, page=64, lens=[500, 0, 77], M=520, rows=[129, 520, 300])),
+    ("bf16", dict(B=2, H=4, Hkv=2, Dh=128, page=32, lens=[900, 333], M=700, rows=[700, 413])),
+    ("bf16", dict(B=3, H=3, Hkv=3, Dh=64, page=64, lens=[500, 0, 77], M=520, rows=[129, 520, 300]))])
+def test_long_chunks(dtype, kw):
+    """Several blocks of rows, the last not whole, over keys of which most blocks see a part."""
+    Case(dtype=dtype, seed=90, **kw).run()
